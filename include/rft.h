@@ -57,7 +57,7 @@
 extern "C" {
 #endif
 
-#define RFT_ABI_VERSION 7
+#define RFT_ABI_VERSION 8
 
 typedef enum {
   RFT_OK = 0,
@@ -442,6 +442,197 @@ rft_status rft_dpo_loss_fwd(const rft_tokens* tok, int64_t V, const float* logp,
                             const float* ref_logp, float beta, float label_smoothing,
                             float* grad_logp, float* seq_logp, rft_dpo_stats* stats, void* ws,
                             size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------- router and weight updates --
+ * What a trainer step needs beside the head's loss and backward: the router of
+ * a mixture-of-experts policy with its auxiliary losses, and the update of the
+ * weights from the gradients. */
+
+/* Over what rft_router_fwd balances the load of the experts. */
+typedef enum {
+  RFT_BALANCE_BATCH = 0,   /* all unmasked rows of the call                           */
+  RFT_BALANCE_ROLLOUT = 1  /* each rollout by itself, then the mean of the rollouts
+                              that have an unmasked row                              */
+} rft_balance_scope;
+
+/* (host struct) Router parameters, the same for the forward and the backward. */
+typedef struct {
+  int32_t n_experts;   /* E, 1 <= E <= 1024                                       */
+  int32_t top_k;       /* k, 1 <= k <= min(E, 16)                                 */
+  int32_t norm_topk;   /* != 0: a row's gates are divided by their sum            */
+  int32_t scope;       /* rft_balance_scope                                       */
+  float balance_coef;  /* c_b >= 0, finite                                        */
+  float z_coef;        /* c_z >= 0, finite                                        */
+} rft_router_params;
+
+/* (device struct) losses and metrics written by rft_router_fwd. */
+typedef struct {
+  float loss;          /* c_b balance_loss + c_z z_loss                            */
+  float balance_loss;  /* E sum_e f_e P_e (1 when the load is even)                */
+  float z_loss;        /* mean over unmasked rows of lse^2                         */
+  int32_t max_count;   /* largest count of an expert (over one group)              */
+  int32_t n_valid;     /* unmasked rows N                                          */
+  int32_t n_groups;    /* rollouts with an unmasked row (RFT_BALANCE_BATCH: 1, 0 if N = 0) */
+} rft_router_stats;
+
+/* Router of a mixture-of-experts layer over the rows of a batch: p = softmax of
+ * the row's E logits, the k experts with the largest logits (equal logits: the
+ * lower index first), their gates, and the load-balance loss of the layer with
+ * a z-loss (an auxiliary loss of the trainer step, added to those above by the
+ * caller).  Of tok, only T, n_seq, seq_start and mask are read (token_ids may be
+ * NULL); here mask is the rows to route, so a padded batch whose prompt rows
+ * are routed too passes its attention mask.
+ * With counts_e the number of rows of a group (the batch, or a rollout) that
+ * selected e and n its unmasked rows,
+ *   f_e = counts_e / (k n), P_e = (1 / n) sum_t p_te,
+ *   balance_loss = E sum_e f_e P_e (RFT_BALANCE_ROLLOUT: the mean over groups).
+ * logits [T, E] in `dtype` with rows ld elements apart (ld >= E; any alignment
+ * of the element type).  A logit below -2e38 (-inf, or a type's lowest value)
+ * excludes its expert from the row: p = 0, never selected; a row with fewer
+ * than k experts left has id -1 and gate 0 in the places after them, and one
+ * with none adds nothing to counts, P and the z-loss (its lse is 0) but counts in n.
+ * A NaN logit makes the row's p, gates and lse NaN; its expert is not selected.
+ * Outputs: expert_ids [T, k] int32 by descending logit, gates [T, k] f32; and,
+ * all or none of them (NULL: routing alone, as for serving; then lse may be
+ * given or NULL and the workspace NULL): lse [T] f32, counts [G, E] int32,
+ * dprob [G, E] f32 = E f_e / n, the gradient of the group's E sum_e f_e P_e to
+ * p_te of its rows (f_e taken as a constant), *stats, with G = 1 or n_seq by scope
+ * (n_seq up to 2^26 by rollout).  Masked rows have id -1
+ * and 0 elsewhere.  A caller that balances over more than this call (other
+ * ranks, other micro-batches) writes its own dprob from the summed counts before
+ * the backward.  Sums over rows run in a fixed order, in fp64 across blocks.
+ * Workspace: rft_router_workspace_bytes().
+ * Errors: RFT_E_NULL, RFT_E_SHAPE, RFT_E_DTYPE, RFT_E_PARAM, RFT_E_WORKSPACE. */
+size_t rft_router_workspace_bytes(const rft_tokens* tok, const rft_router_params* params);
+rft_status rft_router_fwd(const rft_tokens* tok, const void* logits, int dtype, int64_t ld,
+                          const rft_router_params* params, int32_t* expert_ids, float* gates,
+                          float* lse, int32_t* counts, float* dprob, rft_router_stats* stats,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of the router to its logits: of the layers behind it through the gates
+ * (d_gates [T, k] f32; NULL: none; places with id -1 are ignored), and of
+ * c_b balance_loss + c_z z_loss.  With s_j the gates' gradient taken to the
+ * probabilities (norm_topk: (d_gates_j - sum_i d_gates_i gate_i) / sum of the
+ * selected p),
+ *   g_e = c_b / n_groups dprob_e + [e selected at j] s_j,
+ *   d_logits_e = p_e (g_e - sum_i p_i g_i) + 2 c_z lse / n_valid p_e.
+ * logits, expert_ids, lse, dprob and stats as the forward had and wrote them
+ * (ids outside [0, E) are places without an expert).  d_logits [T, E] in `dtype`,
+ * rows ldd elements apart; masked rows and excluded experts get 0.  d_logits may be
+ * logits itself.  Errors: as rft_router_fwd. */
+rft_status rft_router_bwd(const rft_tokens* tok, const void* logits, int dtype, int64_t ld,
+                          const rft_router_params* params, const int32_t* expert_ids,
+                          const float* lse, const float* d_gates, const float* dprob,
+                          const rft_router_stats* stats, void* d_logits, int64_t ldd,
+                          void* stream);
+
+/* (host struct holding device pointers) One tensor of an update, n contiguous
+ * elements in each array, any alignment of its element type. */
+typedef struct {
+  void* weight;      /* weight dtype, updated in place                            */
+  const void* grad;  /* gradient dtype                                            */
+  float* m;          /* first moment, updated in place                            */
+  float* v;          /* second moment, updated in place                           */
+  float* master;     /* fp32 weights, updated in place (weight is then their
+                        rounding), or NULL: weight itself is updated              */
+  int64_t n;
+} rft_param;
+
+/* (device struct) Norm of the gradients and the factor that clips it, written by
+ * rft_grad_norm and read by the updates. */
+typedef struct {
+  float norm;      /* sqrt of the sum of squares over every tensor                 */
+  float scale;     /* max_norm / norm if norm > max_norm > 0, else 1               */
+  int32_t finite;  /* 0: a gradient is inf or NaN; the updates then change nothing */
+} rft_clip;
+
+/* Global 2-norm of the gradients of n_params tensors (params: host array; only
+ * grad and n are read), summed in fp64 in a fixed order.  max_norm = 0: no
+ * clipping.  Workspace: rft_grad_norm_workspace_bytes().
+ * Errors: RFT_E_NULL, RFT_E_SHAPE, RFT_E_DTYPE, RFT_E_PARAM, RFT_E_WORKSPACE. */
+size_t rft_grad_norm_workspace_bytes(const rft_param* params, int64_t n_params);
+rft_status rft_grad_norm(const rft_param* params, int64_t n_params, int grad_dtype,
+                         float max_norm, rft_clip* clip, void* ws, size_t ws_bytes, void* stream);
+
+/* (host struct) AdamW parameters. */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay; /* 0 <= beta < 1, eps >= 0             */
+  int64_t step;                               /* >= 1: of the bias corrections     */
+} rft_adamw_params;
+
+/* One AdamW step over n_params tensors (host array), in place, fp32 arithmetic:
+ *   g = scale grad, m = beta1 m + (1 - beta1) g, v = beta2 v + (1 - beta2) g^2,
+ *   w = w (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * with w the master where given, else the weight in its own type.  clip (device,
+ * may be NULL: scale 1): as rft_grad_norm wrote it; with clip->finite == 0
+ * nothing changes.  Arrays of different tensors may not overlap.
+ * Errors: RFT_E_NULL, RFT_E_SHAPE, RFT_E_DTYPE, RFT_E_PARAM. */
+rft_status rft_adamw_step(const rft_param* params, int64_t n_params, int weight_dtype,
+                          int grad_dtype, const rft_adamw_params* hyper, const rft_clip* clip,
+                          void* stream);
+
+/* (host struct) A stack of `batch` matrices [rows, cols]; every array of a call
+ * has this layout: rows row_stride >= cols elements apart, matrices batch_stride
+ * apart (at least a matrix's extent; not used when batch == 1).  Elements between rows
+ * and matrices are neither read nor written.  Any alignment of the element type. */
+typedef struct {
+  int64_t batch, rows, cols, row_stride, batch_stride;
+} rft_matrices;
+
+/* Matrix products of the orthogonalisation. */
+typedef enum {
+  RFT_PRODUCTS_BY_TYPE = 0, /* fp32 result (out, or weight or master): RFT_PRODUCTS_THREE,
+                               else RFT_PRODUCTS_ONE                                */
+  RFT_PRODUCTS_ONE = 1,     /* operands rounded to fp16, fp32 sums: errors of about 1e-3
+                               (2-norm of the result), below those of a bf16 result  */
+  RFT_PRODUCTS_THREE = 3    /* operands as sums of two fp16 values, three products:
+                               errors as of fp32 products                           */
+} rft_products;
+
+/* (host struct) Parameters of the orthogonalised update. */
+typedef struct {
+  double lr, momentum, weight_decay; /* rft_muon_step only; 0 <= momentum < 1       */
+  double scale;                      /* factor of the orthogonalised matrix         */
+  double a, b, c;                    /* x -> a x + b x^3 + c x^5 (singular values)   */
+  double eps;                        /* >= 0                                        */
+  int32_t steps;                     /* 1 .. 32                                     */
+  int32_t nesterov;                  /* rft_muon_step only                          */
+  int32_t products;                  /* rft_products                                */
+} rft_muon_params;
+
+/* Newton-Schulz orthogonalisation of each matrix of the stack:
+ *   X = G / (|G|_F + eps), then `steps` times A = X X^T, X = a X + (b A + c A^2) X
+ * (on G^T when rows > cols), out = scale X.  a, b, c have to keep the singular
+ * values, which start in [0, 1], below 4 and b A + c A^2 within 15 throughout (3.4445,
+ * -4.7750, 2.0315 do): larger ones may overflow to inf or NaN.  A matrix of zeros
+ * gives zeros, one with an inf or NaN gives NaN (and leaves the others alone).
+ * g in `dtype`, out in `out_dtype` (out may be g when the types agree).
+ * Workspace: rft_orthogonalize_workspace_bytes() with the same mats, params and
+ * out_dtype.  The result does not depend on the workspace's contents.
+ * Errors: RFT_E_NULL, RFT_E_SHAPE (batch < 0, rows or cols < 1, strides; the
+ * smaller side at most 16384, the larger at most 2^20), RFT_E_DTYPE, RFT_E_PARAM,
+ * RFT_E_WORKSPACE. */
+size_t rft_orthogonalize_workspace_bytes(const rft_matrices* mats, const rft_muon_params* params,
+                                         int out_dtype);
+rft_status rft_orthogonalize(const rft_matrices* mats, const void* g, int dtype,
+                             const rft_muon_params* params, void* out, int out_dtype, void* ws,
+                             size_t ws_bytes, void* stream);
+
+/* One step of momentum with an orthogonalised update, in place:
+ *   buf = momentum buf + (1 - momentum) grad,
+ *   u = nesterov ? momentum buf + (1 - momentum) grad : buf,
+ *   w = w (1 - lr weight_decay) - lr scale O,  O as rft_orthogonalize makes it of u,
+ * with w the master (fp32) where given, else the weight in its own type, and the
+ * weight then the rounding of the master.  momentum_buf f32; NULL: u = grad (and
+ * momentum is ignored).  clip (device, may be NULL): grad is scaled by clip->scale
+ * first, and with clip->finite == 0 nothing changes.
+ * Workspace: rft_orthogonalize_workspace_bytes() with out_dtype RFT_F32 when a
+ * master is given, else the weight's.
+ * Errors: as rft_orthogonalize. */
+rft_status rft_muon_step(const rft_matrices* mats, const void* grad, int grad_dtype,
+                         float* momentum_buf, void* weight, int weight_dtype, float* master,
+                         const rft_muon_params* params, const rft_clip* clip, void* ws,
+                         size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -23,6 +23,8 @@ RFT_OK, RFT_E_NULL, RFT_E_SHAPE, RFT_E_DTYPE, RFT_E_PARAM, RFT_E_WORKSPACE, \
 RFT_F32, RFT_BF16 = 0, 1
 RFT_AGG_SEQ_MEAN_TOKEN_MEAN, RFT_AGG_TOKEN_MEAN = 0, 1
 RFT_ADV_GRPO, RFT_ADV_MEAN_CENTER, RFT_ADV_LEAVE_ONE_OUT = 0, 1, 2
+RFT_BALANCE_BATCH, RFT_BALANCE_ROLLOUT = 0, 1
+RFT_PRODUCTS_BY_TYPE, RFT_PRODUCTS_ONE, RFT_PRODUCTS_THREE = 0, 1, 3
 (RFT_OP_TOKEN_LOGPROBS, RFT_OP_TOKEN_LOGPROBS_FROM_LOGITS, RFT_OP_PPO_FWD, RFT_OP_PPO_BWD,
  RFT_OP_PPO_BWD_LOGITS, RFT_OP_PPO_FUSED_LOGITS, RFT_OP_PPO_STEP, RFT_OP_SFT_FWD,
  RFT_OP_DPO_FWD) = range(9)
@@ -58,6 +60,44 @@ class rft_dpo_stats(ctypes.Structure):
                 ("rejected_reward", ctypes.c_double), ("reward_acc", ctypes.c_double),
                 ("margin_mean", ctypes.c_double), ("n_pairs", ctypes.c_int64),
                 ("n_valid", ctypes.c_int64), ("n_bad_ids", ctypes.c_int64)]
+
+
+class rft_router_params(ctypes.Structure):
+    _fields_ = [("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("norm_topk", ctypes.c_int32), ("scope", ctypes.c_int32),
+                ("balance_coef", ctypes.c_float), ("z_coef", ctypes.c_float)]
+
+
+class rft_router_stats(ctypes.Structure):
+    _fields_ = [("loss", ctypes.c_float), ("balance_loss", ctypes.c_float),
+                ("z_loss", ctypes.c_float), ("max_count", ctypes.c_int32),
+                ("n_valid", ctypes.c_int32), ("n_groups", ctypes.c_int32)]
+
+
+class rft_param(ctypes.Structure):
+    _fields_ = [("weight", _p), ("grad", _p), ("m", _p), ("v", _p), ("master", _p), ("n", _i64)]
+
+
+class rft_clip(ctypes.Structure):
+    _fields_ = [("norm", ctypes.c_float), ("scale", ctypes.c_float), ("finite", ctypes.c_int32)]
+
+
+class rft_adamw_params(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", _i64)]
+
+
+class rft_matrices(ctypes.Structure):
+    _fields_ = [("batch", _i64), ("rows", _i64), ("cols", _i64), ("row_stride", _i64),
+                ("batch_stride", _i64)]
+
+
+class rft_muon_params(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("scale", ctypes.c_double),
+                ("a", ctypes.c_double), ("b", ctypes.c_double), ("c", ctypes.c_double),
+                ("eps", ctypes.c_double), ("steps", ctypes.c_int32), ("nesterov", ctypes.c_int32),
+                ("products", ctypes.c_int32)]
 
 
 STATS_BYTES = ctypes.sizeof(rft_ppo_stats)
@@ -107,6 +147,28 @@ _SIGS = {
                                         ctypes.c_double, _p, _p, _p, ctypes.c_size_t, _p]),
     "rft_dpo_loss_fwd": (ctypes.c_int, [ctypes.POINTER(rft_tokens), _i64, _p, _p, ctypes.c_float,
                                         ctypes.c_float, _p, _p, _p, _p, ctypes.c_size_t, _p]),
+    "rft_router_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(rft_tokens),
+                                                     ctypes.POINTER(rft_router_params)]),
+    "rft_router_fwd": (ctypes.c_int, [ctypes.POINTER(rft_tokens), _p, ctypes.c_int, _i64,
+                                      ctypes.POINTER(rft_router_params), _p, _p, _p, _p, _p, _p,
+                                      _p, ctypes.c_size_t, _p]),
+    "rft_router_bwd": (ctypes.c_int, [ctypes.POINTER(rft_tokens), _p, ctypes.c_int, _i64,
+                                      ctypes.POINTER(rft_router_params), _p, _p, _p, _p, _p, _p,
+                                      _i64, _p]),
+    "rft_grad_norm_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(rft_param), _i64]),
+    "rft_grad_norm": (ctypes.c_int, [ctypes.POINTER(rft_param), _i64, ctypes.c_int, ctypes.c_float,
+                                     _p, _p, ctypes.c_size_t, _p]),
+    "rft_adamw_step": (ctypes.c_int, [ctypes.POINTER(rft_param), _i64, ctypes.c_int, ctypes.c_int,
+                                      ctypes.POINTER(rft_adamw_params), _p, _p]),
+    "rft_orthogonalize_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(rft_matrices),
+                                                            ctypes.POINTER(rft_muon_params),
+                                                            ctypes.c_int]),
+    "rft_orthogonalize": (ctypes.c_int, [ctypes.POINTER(rft_matrices), _p, ctypes.c_int,
+                                         ctypes.POINTER(rft_muon_params), _p, ctypes.c_int, _p,
+                                         ctypes.c_size_t, _p]),
+    "rft_muon_step": (ctypes.c_int, [ctypes.POINTER(rft_matrices), _p, ctypes.c_int, _p, _p,
+                                     ctypes.c_int, _p, ctypes.POINTER(rft_muon_params), _p, _p,
+                                     ctypes.c_size_t, _p]),
 }
 
 _LIB = None
@@ -164,11 +226,11 @@ def _dtype_code(t):
 
 @dataclass
 class Tokens:
-    """Token layout of one batch: rollout row offsets, action mask, sampled ids,
-    and optionally per-rollout expert flags (MIX)."""
+    """Token layout of one batch: rollout row offsets, action mask, sampled ids
+    (not needed by the router), and optionally per-rollout expert flags (MIX)."""
     seq_start: torch.Tensor   # int32 [n_seq + 1]
     mask: torch.Tensor        # uint8 [T]
-    token_ids: torch.Tensor   # int32 [T]
+    token_ids: torch.Tensor = None  # int32 [T]
     is_expert: torch.Tensor = None  # uint8 [n_seq] or None
 
     @property
@@ -182,6 +244,8 @@ class Tokens:
     def c(self) -> rft_tokens:
         for t, dt in ((self.seq_start, torch.int32), (self.mask, torch.uint8),
                       (self.token_ids, torch.int32)):
+            if t is None and t is self.token_ids:
+                continue
             if t.dtype != dt or not t.is_contiguous():
                 raise TypeError("tokens: seq_start int32, mask uint8, token_ids int32, contiguous")
         ex = None
@@ -190,8 +254,9 @@ class Tokens:
                     or self.is_expert.numel() != self.n_seq):
                 raise TypeError("tokens: is_expert must be contiguous uint8 [n_seq]")
             ex = self.is_expert.data_ptr()
+        ids = None if self.token_ids is None else self.token_ids.data_ptr()
         return rft_tokens(self.T, self.n_seq, self.seq_start.data_ptr(), self.mask.data_ptr(),
-                          self.token_ids.data_ptr(), ex)
+                          ids, ex)
 
 
 def ppo_params(eps_low=0.2, eps_high=0.2, kl_coef=0.0, agg=RFT_AGG_SEQ_MEAN_TOKEN_MEAN,
@@ -430,6 +495,300 @@ def rft_dpo_loss_fwd(tokens: Tokens, V, logp, ref_logp, beta=0.1, label_smoothin
                                   label_smoothing, _ptr(grad_logp), _ptr(seq_logp), _ptr(stats),
                                   _ptr(ws), nb, _stream(stream)))
     return grad_logp, seq_logp, stats
+
+
+def _stream_of(t, stream):
+    """The given stream, or the current one of the tensor's device."""
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+
+
+def _used_on(stream, *ts):
+    """Tells the allocator that arrays made here are used on a given stream, not on the
+    current one that they were allocated on (they may be freed before the work is done)."""
+    if stream is not None:
+        for t in ts:
+            if t is not None and t.numel():
+                t.record_stream(stream)
+
+
+def _want(t, dtype, shape, name):
+    """A given array of a call: the dtype and shape that the entry point assumes, contiguous."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise TypeError(f"{name}: contiguous {dtype} {tuple(shape)} expected, "
+                        f"got {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def _same_device(dev, *named):
+    for name, t in named:
+        if t is not None and t.device != dev:
+            raise RuntimeError(f"{name} is on {t.device}, the call works on {dev}")
+
+
+# ------------------------------------------------------------------ router --
+def router_params(n_experts, top_k, norm_topk=True, scope=RFT_BALANCE_BATCH, balance_coef=0.0,
+                  z_coef=0.0) -> rft_router_params:
+    return rft_router_params(n_experts, top_k, 1 if norm_topk else 0, scope, balance_coef, z_coef)
+
+
+@dataclass
+class RouterOut:
+    """Outputs of rft_router_fwd; lse, counts, dprob and stats are None without the loss."""
+    expert_ids: torch.Tensor      # int32 [T, k]
+    gates: torch.Tensor           # f32 [T, k]
+    lse: torch.Tensor = None      # f32 [T]
+    counts: torch.Tensor = None   # int32 [G, E]
+    dprob: torch.Tensor = None    # f32 [G, E]
+    stats: torch.Tensor = None    # rft_router_stats (uint8), see stats_to_dict
+
+    @property
+    def losses(self):
+        """[loss, balance_loss, z_loss] as a view of the statistics (device, f32)."""
+        return self.stats[:12].view(torch.float32)
+
+
+def _router_rows(tokens, logits, params, name):
+    T, E = tokens.T, params.n_experts
+    if logits.dim() != 2 or logits.shape != (T, E) or (T and E > 1 and logits.stride(1) != 1):
+        raise TypeError(f"{name}: [{T}, {E}] with unit column stride expected, got "
+                        f"{tuple(logits.shape)} strides {logits.stride()}")
+    # one row, or a broadcast one, has a stride of its own kind; the library reads T of them
+    ld = logits.stride(0) if T > 1 else E
+    return _dtype_code(logits), ld
+
+
+def rft_router_fwd(tokens: Tokens, logits, params, want_loss=True, out=None, ws=None, stream=None):
+    """Returns a RouterOut; `out` (one of an earlier call with the same sizes) is written anew."""
+    _need_gpu(logits, tokens.mask, tokens.seq_start)
+    dev, T, k = logits.device, tokens.T, params.top_k
+    _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start), ("ws", ws))
+    dt, ld = _router_rows(tokens, logits, params, "logits")
+    G = tokens.n_seq if params.scope == RFT_BALANCE_ROLLOUT else 1
+    E = params.n_experts
+    if out is None:
+        out = RouterOut(torch.empty((T, k), dtype=torch.int32, device=dev),
+                        torch.empty((T, k), dtype=torch.float32, device=dev))
+        if want_loss:
+            out.lse = torch.empty(T, dtype=torch.float32, device=dev)
+            out.counts = torch.empty((G, E), dtype=torch.int32, device=dev)
+            out.dprob = torch.empty((G, E), dtype=torch.float32, device=dev)
+            out.stats = torch.empty(ctypes.sizeof(rft_router_stats), dtype=torch.uint8, device=dev)
+    else:
+        _want(out.expert_ids, torch.int32, (T, k), "expert_ids")
+        _want(out.gates, torch.float32, (T, k), "gates")
+        if want_loss:
+            _want(out.lse, torch.float32, (T,), "lse")
+            _want(out.counts, torch.int32, (G, E), "counts")
+            _want(out.dprob, torch.float32, (G, E), "dprob")
+            _want(out.stats, torch.uint8, (ctypes.sizeof(rft_router_stats),), "stats")
+        _same_device(dev, ("out", out.expert_ids), ("out", out.gates))
+    tk = tokens.c()
+    nb = 0
+    o = out if want_loss else RouterOut(out.expert_ids, out.gates)
+    if want_loss:
+        need = int(lib().rft_router_workspace_bytes(ctypes.byref(tk), ctypes.byref(params)))
+        ws, nb = _workspace(need, dev, ws)
+    with torch.cuda.device(dev):
+        _check(lib().rft_router_fwd(ctypes.byref(tk), _ptr(logits), dt, ld, ctypes.byref(params),
+                                    _ptr(o.expert_ids), _ptr(o.gates), _ptr(o.lse), _ptr(o.counts),
+                                    _ptr(o.dprob), _ptr(o.stats), _ptr(ws), nb,
+                                    _stream_of(logits, stream)))
+    _used_on(stream, out.expert_ids, out.gates, o.lse, o.counts, o.dprob, o.stats, ws)
+    return out
+
+
+def rft_router_bwd(tokens: Tokens, logits, params, fwd: RouterOut, d_gates=None, d_logits=None,
+                   stream=None):
+    """Returns d_logits; `fwd` is what rft_router_fwd returned for the same inputs."""
+    _need_gpu(logits, tokens.mask, tokens.seq_start)
+    dev, T, k = logits.device, tokens.T, params.top_k
+    dt, ld = _router_rows(tokens, logits, params, "logits")
+    if d_gates is not None:
+        _want(d_gates, torch.float32, (T, k), "d_gates")
+    if fwd.stats is None:
+        raise TypeError("rft_router_bwd needs a forward with want_loss=True")
+    _want(fwd.expert_ids, torch.int32, (T, k), "expert_ids")
+    _want(fwd.lse, torch.float32, (T,), "lse")
+    G = tokens.n_seq if params.scope == RFT_BALANCE_ROLLOUT else 1
+    _want(fwd.dprob, torch.float32, (G, params.n_experts), "dprob")
+    if d_logits is None:
+        d_logits = torch.empty((T, params.n_experts), dtype=logits.dtype, device=dev)
+    if d_logits.dtype != logits.dtype:
+        raise TypeError("d_logits has the dtype of logits")
+    _, ldd = _router_rows(tokens, d_logits, params, "d_logits")
+    if T > 1 and ldd < params.n_experts:
+        raise TypeError("d_logits: rows overlap")
+    _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start), ("d_gates", d_gates),
+                 ("expert_ids", fwd.expert_ids), ("d_logits", d_logits), ("stats", fwd.stats))
+    tk = tokens.c()
+    with torch.cuda.device(dev):
+        _check(lib().rft_router_bwd(ctypes.byref(tk), _ptr(logits), dt, ld, ctypes.byref(params),
+                                    _ptr(fwd.expert_ids), _ptr(fwd.lse), _ptr(d_gates),
+                                    _ptr(fwd.dprob), _ptr(fwd.stats), _ptr(d_logits), ldd,
+                                    _stream_of(logits, stream)))
+    _used_on(stream, d_logits)
+    return d_logits
+
+
+# ----------------------------------------------------------------- updates --
+class Params:
+    """Tensors of an update as (weight, grad, m, v[, master]) tuples, all contiguous and of one
+    size each; a training program makes it once and keeps it.  For rft_grad_norm alone weight,
+    m and v may be None."""
+
+    def __init__(self, tensors):
+        self.tensors = [tuple(t) + (None,) * (5 - len(t)) for t in tensors]
+        self.device = None
+        self.weight_dtype = self.grad_dtype = None
+        self.masters = any(t[4] is not None for t in self.tensors)
+        self.c = (rft_param * max(1, len(self.tensors)))()
+        for i, (w, g, m, v, master) in enumerate(self.tensors):
+            _need_gpu(w, g, m, v, master)
+            self.device = self.device or g.device
+            self.grad_dtype = self.grad_dtype or g.dtype
+            if w is not None:
+                self.weight_dtype = self.weight_dtype or w.dtype
+            for name, t, dt in (("weight", w, self.weight_dtype), ("grad", g, self.grad_dtype),
+                                ("m", m, torch.float32), ("v", v, torch.float32),
+                                ("master", master, torch.float32)):
+                if t is None:
+                    continue
+                if t.dtype != dt or t.numel() != g.numel() or not t.is_contiguous():
+                    raise TypeError(f"tensor {i}: {name} must be contiguous {dt} of "
+                                    f"{g.numel()} elements")
+                if t.device != self.device:
+                    raise RuntimeError(f"tensor {i}: {name} is on {t.device}, not {self.device}")
+            self.c[i] = rft_param(*(None if t is None else t.data_ptr()
+                                    for t in (w, g, m, v, master)), g.numel())
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+class Clip:
+    """Gradient norm and clip factor on the device (rft_clip)."""
+
+    def __init__(self, device):
+        self.buf = torch.empty(ctypes.sizeof(rft_clip), dtype=torch.uint8, device=device)
+
+    @property
+    def norm(self):
+        return self.buf[:4].view(torch.float32)[0]
+
+    @property
+    def scale(self):
+        return self.buf[4:8].view(torch.float32)[0]
+
+    @property
+    def finite(self):
+        return self.buf[8:12].view(torch.int32)[0]
+
+
+def _code(dtype):
+    if dtype == torch.bfloat16:
+        return RFT_BF16
+    if dtype == torch.float32 or dtype is None:
+        return RFT_F32
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def rft_grad_norm(params: Params, max_norm=0.0, clip=None, ws=None, stream=None) -> Clip:
+    """Global gradient norm; the returned Clip feeds rft_adamw_step and rft_muon_step."""
+    dev = params.device or torch.device("cuda", torch.cuda.current_device())
+    clip = Clip(dev) if clip is None else clip
+    _same_device(dev, ("clip", clip.buf), ("ws", ws))
+    need = int(lib().rft_grad_norm_workspace_bytes(params.c, len(params)))
+    ws, nb = _workspace(need, dev, ws)
+    with torch.cuda.device(dev):
+        _check(lib().rft_grad_norm(params.c, len(params), _code(params.grad_dtype), max_norm,
+                                   _ptr(clip.buf), _ptr(ws), nb, _stream_of(clip.buf, stream)))
+    _used_on(stream, clip.buf, ws)
+    return clip
+
+
+def adamw_params(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
+                 step=1) -> rft_adamw_params:
+    return rft_adamw_params(lr, beta1, beta2, eps, weight_decay, step)
+
+
+def rft_adamw_step(params: Params, hyper, clip=None, stream=None):
+    """One AdamW step in place over every tensor of `params`."""
+    dev = params.device or torch.device("cuda", torch.cuda.current_device())
+    _same_device(dev, ("clip", clip.buf if clip is not None else None))
+    with torch.cuda.device(dev):
+        s = torch.cuda.current_stream(dev) if stream is None else stream
+        _check(lib().rft_adamw_step(params.c, len(params), _code(params.weight_dtype),
+                                    _code(params.grad_dtype), ctypes.byref(hyper),
+                                    _ptr(clip.buf) if clip is not None else None,
+                                    ctypes.c_void_p(s.cuda_stream)))
+
+
+def muon_params(lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0, steps=5,
+                coefs=(3.4445, -4.7750, 2.0315), eps=1e-7,
+                products=RFT_PRODUCTS_BY_TYPE) -> rft_muon_params:
+    return rft_muon_params(lr, momentum, weight_decay, scale, *coefs, eps, steps,
+                           1 if nesterov else 0, products)
+
+
+def _matrices(first, *others):
+    """The layout [rows, cols] or [batch, rows, cols] that every array of a call shares."""
+    name, t = first
+    if t.dim() not in (2, 3) or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise TypeError(f"{name}: [rows, cols] or [batch, rows, cols] with unit column stride")
+    b = t.shape[0] if t.dim() == 3 else 1
+    r, c = t.shape[-2:]
+    # the strides that move: of several rows, and of several matrices
+    key = lambda x: ((x.stride(-2) if r > 1 else c),  # noqa: E731
+                     (x.stride(0) if x.dim() == 3 and b > 1 else 0))
+    for n, x in others:
+        if x is None:
+            continue
+        if x.shape != t.shape or (c > 1 and x.stride(-1) != 1) or key(x) != key(t):
+            raise TypeError(f"{n}: the shape and strides of {name} expected")
+        if x.device != t.device:
+            raise RuntimeError(f"{n} is on {x.device}, {name} on {t.device}")
+    return rft_matrices(b, r, c, *key(t))
+
+
+def rft_orthogonalize(g, params, out=None, out_dtype=None, ws=None, stream=None):
+    """Orthogonalises [rows, cols] or each of [batch, rows, cols]; out has g's strides."""
+    _need_gpu(g, out)
+    if out is None:
+        out = torch.empty_strided(g.shape, g.stride(), dtype=out_dtype or g.dtype, device=g.device)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError("out has another dtype than out_dtype")
+    mats = _matrices(("g", g), ("out", out))
+    _same_device(g.device, ("ws", ws))
+    dt, odt = _dtype_code(g), _dtype_code(out)
+    need = int(lib().rft_orthogonalize_workspace_bytes(ctypes.byref(mats), ctypes.byref(params), odt))
+    ws, nb = _workspace(need, g.device, ws)
+    with torch.cuda.device(g.device):
+        _check(lib().rft_orthogonalize(ctypes.byref(mats), _ptr(g), dt, ctypes.byref(params),
+                                       _ptr(out), odt, _ptr(ws), nb, _stream_of(g, stream)))
+    _used_on(stream, out, ws)
+    return out
+
+
+def rft_muon_step(weight, grad, momentum, params, master=None, clip=None, ws=None, stream=None):
+    """One orthogonalised momentum step in place; every array has the weight's strides."""
+    _need_gpu(weight, grad, momentum, master)
+    mats = _matrices(("weight", weight), ("grad", grad), ("momentum", momentum), ("master", master))
+    for name, t in (("momentum", momentum), ("master", master)):
+        if t is not None and t.dtype != torch.float32:
+            raise TypeError(f"{name} is float32")
+    _same_device(weight.device, ("ws", ws), ("clip", clip.buf if clip is not None else None))
+    wdt, gdt = _dtype_code(weight), _dtype_code(grad)
+    need = int(lib().rft_orthogonalize_workspace_bytes(
+        ctypes.byref(mats), ctypes.byref(params), RFT_F32 if master is not None else wdt))
+    ws, nb = _workspace(need, weight.device, ws)
+    with torch.cuda.device(weight.device):
+        _check(lib().rft_muon_step(ctypes.byref(mats), _ptr(grad), gdt, _ptr(momentum),
+                                   _ptr(weight), wdt, _ptr(master), ctypes.byref(params),
+                                   _ptr(clip.buf) if clip is not None else None, _ptr(ws), nb,
+                                   _stream_of(weight, stream)))
+    _used_on(stream, ws)
 
 
 def loaded_library_path() -> str:

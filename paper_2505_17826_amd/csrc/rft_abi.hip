@@ -10,13 +10,13 @@
 #include <mutex>
 #include <string>
 
-#include "rft_internal.h"
+#include "abi_common.h"
 
 using namespace rft;
 
-namespace {
+namespace rft {
 
-thread_local std::string g_err;
+static thread_local std::string g_err;
 
 rft_status fail(rft_status s, const char* fmt, ...) {
   char buf[512];
@@ -32,15 +32,17 @@ rft_status hip_fail(hipError_t e, const char* where) {
   return fail(RFT_E_HIP, "%s: HIP error %d (%s)", where, (int)e, hipGetErrorString(e));
 }
 
-#define RFT_HIP(call, where)                        \
-  do {                                              \
-    hipError_t e_ = (call);                         \
-    if (e_ != hipSuccess) return hip_fail(e_, where); \
-  } while (0)
+rft_status check_ws(const char* fn, void* ws, size_t have, size_t need) {
+  if (need == 0) return RFT_OK;
+  if (!ws) return fail(RFT_E_WORKSPACE, "%s: workspace is NULL (%zu bytes needed)", fn, need);
+  if (!aligned16(ws)) return fail(RFT_E_WORKSPACE, "%s: workspace must be 16-byte aligned", fn);
+  if (have < need) return fail(RFT_E_WORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, have, need);
+  return RFT_OK;
+}
 
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+}  // namespace rft
 
-int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+namespace {
 
 rft_status check_tokens(const rft_tokens* tok, const char* fn) {
   if (!tok) return fail(RFT_E_NULL, "%s: tokens is NULL", fn);
@@ -119,14 +121,6 @@ LossConst loss_const(const rft_ppo_params* p, int64_t V, const rft_tokens& tok) 
   c.is_expert = tok.is_expert;
   c.mix = tok.is_expert ? 1 : 0;
   return c;
-}
-
-rft_status check_ws(const char* fn, void* ws, size_t have, size_t need) {
-  if (need == 0) return RFT_OK;
-  if (!ws) return fail(RFT_E_WORKSPACE, "%s: workspace is NULL (%zu bytes needed)", fn, need);
-  if (!aligned16(ws)) return fail(RFT_E_WORKSPACE, "%s: workspace must be 16-byte aligned", fn);
-  if (have < need) return fail(RFT_E_WORKSPACE, "%s: workspace %zu bytes < %zu needed", fn, have, need);
-  return RFT_OK;
 }
 
 // ---------------------------------------------------- workspace layouts --

@@ -1,0 +1,200 @@
+"""rft_orthogonalize and rft_muon_step against the Newton-Schulz polynomial in float64:
+shapes around the tiles, both orientations, stacks, strides, types, both kinds of
+products, the momentum, masters, clipping and inputs that are not finite."""
+import math
+
+import pytest
+import torch
+
+import paper_2505_17826_amd as R
+from tests.gpu_cases import requires_gpu
+
+pytestmark = [pytest.mark.gpu, requires_gpu]
+DEV = torch.device("cuda")
+COEFS = (3.4445, -4.7750, 2.0315)
+
+
+def polynomial(g, steps=5, coefs=COEFS, eps=1e-7):
+    """The iteration on the singular values, in float64 on the host."""
+    x = g.detach().double().cpu()
+    flip = x.shape[-2] > x.shape[-1]
+    x = x.transpose(-1, -2) if flip else x
+    x = x / (torch.linalg.matrix_norm(x, keepdim=True) + eps)
+    a, b, c = coefs
+    for _ in range(steps):
+        y = x @ x.transpose(-1, -2)
+        x = a * x + (b * y + c * y @ y) @ x
+    return x.transpose(-1, -2) if flip else x
+
+
+def matrix(seed, *shape):
+    """Noise and a few strong directions, as a gradient has."""
+    g = torch.Generator().manual_seed(seed)
+    m, n = shape[-2:]
+    r = min(4, m, n)
+    s = 4 * (math.sqrt(m) + math.sqrt(n)) / math.sqrt(m * n)
+    u = torch.randn(*shape[:-1], r, generator=g)
+    v = torch.randn(*shape[:-2], r, n, generator=g)
+    return torch.randn(*shape, generator=g) + s * u @ v
+
+
+def off(x, ref):
+    d = (x.double().cpu() - ref).flatten(-2).norm(dim=-1)
+    return float((d / ref.flatten(-2).norm(dim=-1)).max())
+
+
+# How far a result may be off (2-norm, relative).  A rounding error made in one step is
+# multiplied in the later ones by at most a^4 = 141 where a singular value is near 0, and by
+# about 1 where it has grown; three products leave 2^-22 of a term per product, one product
+# 2^-11 of the off-diagonal part.  With g's strong directions most directions start small,
+# within the first steps of growth; 2^-22 a^2 sqrt(5) and 2^-11 a^2 / sqrt(5 steps' average of
+# an error spread over all directions, of which the small ones hold a part) are taken whole:
+LIMIT = {R.RFT_PRODUCTS_THREE: 2.0 ** -22 * 141, R.RFT_PRODUCTS_ONE: 2.0 ** -11 * 11.9}
+SHAPES = [(1, 1), (1, 7), (5, 1), (2, 3), (16, 16), (17, 90), (64, 64), (63, 129), (128, 128),
+          (129, 128), (128, 300), (200, 70), (257, 256), (384, 640), (1000, 130), (33, 2050)]
+
+
+@pytest.mark.parametrize("products", [R.RFT_PRODUCTS_ONE, R.RFT_PRODUCTS_THREE])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_shapes(shape, products):
+    g = matrix(shape[0] * 31 + shape[1], *shape)
+    for dt in (torch.float32, torch.bfloat16):
+        x = g.to(dt)
+        ref = polynomial(x)
+        p = R.muon_params(products=products)
+        o = R.rft_orthogonalize(x.to(DEV), p, out_dtype=torch.float32)
+        assert off(o, ref) <= LIMIT[products], off(o, ref)
+        # the bf16 result is the rounding of the same values
+        assert torch.equal(R.rft_orthogonalize(x.to(DEV), p, out_dtype=torch.bfloat16),
+                           o.to(torch.bfloat16))
+
+
+def test_products_by_type():
+    x = matrix(1, 100, 160).to(DEV)
+    for out, same in ((torch.float32, R.RFT_PRODUCTS_THREE), (torch.bfloat16, R.RFT_PRODUCTS_ONE)):
+        a = R.rft_orthogonalize(x, R.muon_params(), out_dtype=out)
+        b = R.rft_orthogonalize(x, R.muon_params(products=same), out_dtype=out)
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shape", [(3, 40, 200), (5, 130, 60), (7, 1, 9), (2, 256, 256)])
+def test_stacks_and_strides(shape):
+    b, m, n = shape
+    x = matrix(b, *shape)
+    x[1] *= 1e-20  # each matrix has its own norm
+    ref = polynomial(x, eps=0.0)
+    p = R.muon_params(eps=0.0, products=R.RFT_PRODUCTS_THREE)
+    whole = R.rft_orthogonalize(x.to(DEV), p)
+    assert off(whole, ref) <= LIMIT[R.RFT_PRODUCTS_THREE]
+    for i in range(b):
+        assert torch.equal(R.rft_orthogonalize(x[i].to(DEV), p), whole[i])
+    # rows and matrices with gaps, from an odd element on: the gaps keep what they held
+    buf = torch.full((b * (m * (n + 3) + 5) + 1,), math.nan, device=DEV)
+    view = torch.as_strided(buf, shape, (m * (n + 3) + 5, n + 3, 1), 1)
+    view.copy_(x)
+    gaps = torch.isnan(buf)
+    o = R.rft_orthogonalize(view, p, out=view)  # in place
+    assert torch.equal(o, whole) and torch.equal(torch.isnan(buf), gaps)
+
+
+def test_steps_coefficients_and_scale():
+    x = matrix(3, 90, 140)
+    for steps in (1, 2, 8):
+        for coefs in (COEFS, (1.5, -0.5, 0.0), (2.0, -1.5, 0.5)):
+            p = R.muon_params(steps=steps, coefs=coefs, scale=0.25, products=R.RFT_PRODUCTS_THREE)
+            o = R.rft_orthogonalize(x.to(DEV), p)
+            assert off(o, 0.25 * polynomial(x, steps, coefs)) <= LIMIT[R.RFT_PRODUCTS_THREE]
+
+
+def test_zero_and_not_finite():
+    x = matrix(4, 4, 130, 150)
+    x[0] = 0
+    x[2, 5, 7] = math.nan
+    x[3, 100, 3] = math.inf
+    for eps in (0.0, 1e-7):
+        o = R.rft_orthogonalize(x.to(DEV), R.muon_params(eps=eps)).cpu()
+        assert bool((o[0] == 0).all()) and bool(torch.isfinite(o[1]).all())
+        assert bool(torch.isnan(o[2]).all()) and bool(torch.isnan(o[3]).all())
+
+
+@pytest.mark.parametrize("wdt,master", [(torch.float32, False), (torch.bfloat16, False),
+                                        (torch.bfloat16, True)])
+@pytest.mark.parametrize("gdt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(70, 200), (300, 129), (3, 64, 40)])
+def test_muon_step(shape, gdt, wdt, master):
+    lr, mu, wd, scale = 0.05, 0.9, 0.1, 1.5
+    for nesterov in (True, False):
+        for with_buf in (True, False):
+            g = matrix(5, *shape).to(gdt)
+            buf = matrix(6, *shape) if with_buf else None
+            w32 = matrix(7, *shape)
+            w = w32.to(wdt)
+            dev = [None if t is None else t.to(DEV) for t in (w, g, buf, w32 if master else None)]
+            prm = R.muon_params(lr, mu, nesterov, wd, scale)
+            R.rft_muon_step(dev[0], dev[1], dev[2], prm, master=dev[3])
+            gd = g.double()
+            if with_buf:
+                b2 = mu * buf.double() + (1 - mu) * gd
+                u = mu * b2 + (1 - mu) * gd if nesterov else b2
+                # two products and a sum, 2^-24 each
+                lim = 3 * 2.0 ** -24 * (buf.double().abs() + gd.abs())
+                assert bool(((dev[2].double().cpu() - b2).abs() <= lim).all())
+            else:
+                u = gd
+            o = lr * scale * polynomial(u)
+            base = (w32 if master else w).double()
+            want = base * (1 - lr * wd) - o
+            got = dev[3] if master else dev[0]
+            one = got.dtype == torch.bfloat16
+            lim = LIMIT[R.RFT_PRODUCTS_ONE if one else R.RFT_PRODUCTS_THREE]
+            d = got.double().cpu() - want
+            rounding = (2.0 ** -8 if one else 3 * 2.0 ** -24) * (base.norm() + o.norm())
+            assert float(d.norm()) <= lim * float(o.norm()) + float(rounding)
+            if master:
+                assert torch.equal(dev[0], dev[3].to(wdt))
+
+
+def test_clip_scales_or_stops_the_step():
+    shape = (60, 100)
+    for bad in (False, True):
+        g = matrix(8, *shape).to(DEV)
+        if bad:
+            g[3, 4] = math.inf
+        buf, w = matrix(9, *shape).to(DEV), matrix(10, *shape).to(DEV)
+        ps = R.Params([(w.view(-1), g.view(-1), buf.view(-1), buf.view(-1))])
+        clip = R.rft_grad_norm(ps, 1.0)
+        b0, w0 = buf.clone(), w.clone()
+        R.rft_muon_step(w, g, buf, R.muon_params(), clip=clip)
+        if bad:
+            assert torch.equal(buf, b0) and torch.equal(w, w0)
+            continue
+        b1, w1 = b0.clone(), w0.clone()
+        R.rft_muon_step(w1, g * clip.scale, b1, R.muon_params())
+        assert torch.equal(buf, b1) and torch.equal(w, w1)
+
+
+def test_same_bits_on_streams_in_graphs_and_whatever_the_workspace_held():
+    x = matrix(11, 2, 150, 260).to(DEV)
+    p = R.muon_params()
+    want = R.rft_orthogonalize(x, p)
+    L = R.lib()
+    import ctypes
+    mats = R.rft_matrices(2, 150, 260, 260, 150 * 260)
+    need = L.rft_orthogonalize_workspace_bytes(ctypes.byref(mats), ctypes.byref(p), R.RFT_F32)
+    for fill in (0, 255, 127):
+        ws = torch.full((need,), fill, dtype=torch.uint8, device=DEV)
+        assert torch.equal(R.rft_orthogonalize(x, p, ws=ws), want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    a = R.rft_orthogonalize(x, p, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(a, want)
+    z = x.clone()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        o = R.rft_orthogonalize(z, p)
+    for i in range(3):
+        z.copy_(x.roll(i, 1))
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, R.rft_orthogonalize(z, p))
