@@ -497,11 +497,27 @@ def rft_dpo_loss_fwd(tokens: Tokens, V, logp, ref_logp, beta=0.1, label_smoothin
     return grad_logp, seq_logp, stats
 
 
-def _stream_of(t, stream):
-    """The given stream, or the current one of the tensor's device."""
-    if stream is not None:
-        return ctypes.c_void_p(stream.cuda_stream)
-    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _call(fn, device, stream, *args):
+    """Runs an entry point with `device` current, on `stream` or the device's current stream;
+    the calls of a decode step take about as long on the host as on the GPU, so the device is
+    set only where it is another one."""
+    i = device.index
+    s = _raw_stream(i) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == i:
+        st = fn(*args, s)
+    else:
+        with torch.cuda.device(i):
+            st = fn(*args, s)
+    if st != RFT_OK:
+        _check(st)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def _used_on(stream, *ts):
@@ -513,12 +529,13 @@ def _used_on(stream, *ts):
                 t.record_stream(stream)
 
 
-def _want(t, dtype, shape, name):
+def _want(dev, t, dtype, shape, name):
     """A given array of a call: the dtype and shape that the entry point assumes, contiguous."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise TypeError(f"{name}: contiguous {dtype} {tuple(shape)} expected, "
                         f"got {t.dtype} {tuple(t.shape)}")
-    return t
+    if t.device != dev:
+        raise RuntimeError(f"{name} is on {t.device}, the call works on {dev}")
 
 
 def _same_device(dev, *named):
@@ -541,93 +558,91 @@ class RouterOut:
     lse: torch.Tensor = None      # f32 [T]
     counts: torch.Tensor = None   # int32 [G, E]
     dprob: torch.Tensor = None    # f32 [G, E]
-    stats: torch.Tensor = None    # rft_router_stats (uint8), see stats_to_dict
+    stats: torch.Tensor = None    # rft_router_stats (held as f32 [6]), see stats_to_dict
 
     @property
     def losses(self):
         """[loss, balance_loss, z_loss] as a view of the statistics (device, f32)."""
-        return self.stats[:12].view(torch.float32)
+        return self.stats[:3]
 
 
-def _router_rows(tokens, logits, params, name):
-    T, E = tokens.T, params.n_experts
-    if logits.dim() != 2 or logits.shape != (T, E) or (T and E > 1 and logits.stride(1) != 1):
+_ROUTER_STATS_WORDS = ctypes.sizeof(rft_router_stats) // 4
+
+
+def _router_rows(T, x, E, name):
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 2 or shape[0] != T or shape[1] != E or (T and E > 1 and stride[1] != 1):
         raise TypeError(f"{name}: [{T}, {E}] with unit column stride expected, got "
-                        f"{tuple(logits.shape)} strides {logits.stride()}")
-    # one row, or a broadcast one, has a stride of its own kind; the library reads T of them
-    ld = logits.stride(0) if T > 1 else E
-    return _dtype_code(logits), ld
+                        f"{tuple(shape)} strides {stride}")
+    # the stride of a single row may be anything
+    return stride[0] if T > 1 else E
 
 
 def rft_router_fwd(tokens: Tokens, logits, params, want_loss=True, out=None, ws=None, stream=None):
     """Returns a RouterOut; `out` (one of an earlier call with the same sizes) is written anew."""
-    _need_gpu(logits, tokens.mask, tokens.seq_start)
-    dev, T, k = logits.device, tokens.T, params.top_k
-    _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start), ("ws", ws))
-    dt, ld = _router_rows(tokens, logits, params, "logits")
-    G = tokens.n_seq if params.scope == RFT_BALANCE_ROLLOUT else 1
-    E = params.n_experts
-    if out is None:
-        out = RouterOut(torch.empty((T, k), dtype=torch.int32, device=dev),
-                        torch.empty((T, k), dtype=torch.float32, device=dev))
-        if want_loss:
-            out.lse = torch.empty(T, dtype=torch.float32, device=dev)
-            out.counts = torch.empty((G, E), dtype=torch.int32, device=dev)
-            out.dprob = torch.empty((G, E), dtype=torch.float32, device=dev)
-            out.stats = torch.empty(ctypes.sizeof(rft_router_stats), dtype=torch.uint8, device=dev)
-    else:
-        _want(out.expert_ids, torch.int32, (T, k), "expert_ids")
-        _want(out.gates, torch.float32, (T, k), "gates")
-        if want_loss:
-            _want(out.lse, torch.float32, (T,), "lse")
-            _want(out.counts, torch.int32, (G, E), "counts")
-            _want(out.dprob, torch.float32, (G, E), "dprob")
-            _want(out.stats, torch.uint8, (ctypes.sizeof(rft_router_stats),), "stats")
-        _same_device(dev, ("out", out.expert_ids), ("out", out.gates))
     tk = tokens.c()
-    nb = 0
-    o = out if want_loss else RouterOut(out.expert_ids, out.gates)
-    if want_loss:
-        need = int(lib().rft_router_workspace_bytes(ctypes.byref(tk), ctypes.byref(params)))
-        ws, nb = _workspace(need, dev, ws)
-    with torch.cuda.device(dev):
-        _check(lib().rft_router_fwd(ctypes.byref(tk), _ptr(logits), dt, ld, ctypes.byref(params),
-                                    _ptr(o.expert_ids), _ptr(o.gates), _ptr(o.lse), _ptr(o.counts),
-                                    _ptr(o.dprob), _ptr(o.stats), _ptr(ws), nb,
-                                    _stream_of(logits, stream)))
-    _used_on(stream, out.expert_ids, out.gates, o.lse, o.counts, o.dprob, o.stats, ws)
+    dev, T, k, E = logits.device, tk.T, params.top_k, params.n_experts
+    _need_gpu(logits)
+    _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start), ("ws", ws))
+    dt, ld = _dtype_code(logits), _router_rows(T, logits, E, "logits")
+    G = tk.n_seq if params.scope == RFT_BALANCE_ROLLOUT else 1
+    i32, f32 = torch.int32, torch.float32
+    if out is None:
+        new = torch.empty
+        out = RouterOut(new((T, k), dtype=i32, device=dev), new((T, k), dtype=f32, device=dev))
+        if want_loss:
+            out.lse = new(T, dtype=f32, device=dev)
+            out.counts = new((G, E), dtype=i32, device=dev)
+            out.dprob = new((G, E), dtype=f32, device=dev)
+            out.stats = new(_ROUTER_STATS_WORDS, dtype=f32, device=dev)
+    else:
+        _want(dev, out.expert_ids, i32, (T, k), "expert_ids")
+        _want(dev, out.gates, f32, (T, k), "gates")
+        if want_loss:
+            _want(dev, out.lse, f32, (T,), "lse")
+            _want(dev, out.counts, i32, (G, E), "counts")
+            _want(dev, out.dprob, f32, (G, E), "dprob")
+            _want(dev, out.stats, f32, (_ROUTER_STATS_WORDS,), "stats")
+    L, rt, rp = lib(), ctypes.byref(tk), ctypes.byref(params)
+    if not want_loss:
+        _call(L.rft_router_fwd, dev, stream, rt, _at(logits), dt, ld, rp, _at(out.expert_ids),
+              _at(out.gates), None, None, None, None, None, 0)
+        _used_on(stream, out.expert_ids, out.gates)
+        return out
+    ws, nb = _workspace(int(L.rft_router_workspace_bytes(rt, rp)), dev, ws)
+    _call(L.rft_router_fwd, dev, stream, rt, _at(logits), dt, ld, rp, _at(out.expert_ids),
+          _at(out.gates), _at(out.lse), _at(out.counts), _at(out.dprob), _at(out.stats), _at(ws), nb)
+    _used_on(stream, out.expert_ids, out.gates, out.lse, out.counts, out.dprob, out.stats, ws)
     return out
 
 
 def rft_router_bwd(tokens: Tokens, logits, params, fwd: RouterOut, d_gates=None, d_logits=None,
                    stream=None):
     """Returns d_logits; `fwd` is what rft_router_fwd returned for the same inputs."""
-    _need_gpu(logits, tokens.mask, tokens.seq_start)
-    dev, T, k = logits.device, tokens.T, params.top_k
-    dt, ld = _router_rows(tokens, logits, params, "logits")
+    tk = tokens.c()
+    dev, T, k, E = logits.device, tk.T, params.top_k, params.n_experts
+    _need_gpu(logits)
+    _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start))
+    dt, ld = _dtype_code(logits), _router_rows(T, logits, E, "logits")
+    f32 = torch.float32
     if d_gates is not None:
-        _want(d_gates, torch.float32, (T, k), "d_gates")
+        _want(dev, d_gates, f32, (T, k), "d_gates")
     if fwd.stats is None:
         raise TypeError("rft_router_bwd needs a forward with want_loss=True")
-    _want(fwd.expert_ids, torch.int32, (T, k), "expert_ids")
-    _want(fwd.lse, torch.float32, (T,), "lse")
-    G = tokens.n_seq if params.scope == RFT_BALANCE_ROLLOUT else 1
-    _want(fwd.dprob, torch.float32, (G, params.n_experts), "dprob")
+    _want(dev, fwd.expert_ids, torch.int32, (T, k), "expert_ids")
+    _want(dev, fwd.lse, f32, (T,), "lse")
+    _want(dev, fwd.dprob, f32, (tk.n_seq if params.scope == RFT_BALANCE_ROLLOUT else 1, E), "dprob")
+    _want(dev, fwd.stats, f32, (_ROUTER_STATS_WORDS,), "stats")
     if d_logits is None:
-        d_logits = torch.empty((T, params.n_experts), dtype=logits.dtype, device=dev)
-    if d_logits.dtype != logits.dtype:
-        raise TypeError("d_logits has the dtype of logits")
-    _, ldd = _router_rows(tokens, d_logits, params, "d_logits")
-    if T > 1 and ldd < params.n_experts:
-        raise TypeError("d_logits: rows overlap")
-    _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start), ("d_gates", d_gates),
-                 ("expert_ids", fwd.expert_ids), ("d_logits", d_logits), ("stats", fwd.stats))
-    tk = tokens.c()
-    with torch.cuda.device(dev):
-        _check(lib().rft_router_bwd(ctypes.byref(tk), _ptr(logits), dt, ld, ctypes.byref(params),
-                                    _ptr(fwd.expert_ids), _ptr(fwd.lse), _ptr(d_gates),
-                                    _ptr(fwd.dprob), _ptr(fwd.stats), _ptr(d_logits), ldd,
-                                    _stream_of(logits, stream)))
+        d_logits, ldd = torch.empty((T, E), dtype=logits.dtype, device=dev), E
+    else:
+        if d_logits.dtype != logits.dtype:
+            raise TypeError("d_logits has the dtype of logits")
+        ldd = _router_rows(T, d_logits, E, "d_logits")
+        _same_device(dev, ("d_logits", d_logits))
+    _call(lib().rft_router_bwd, dev, stream, ctypes.byref(tk), _at(logits), dt, ld,
+          ctypes.byref(params), _at(fwd.expert_ids), _at(fwd.lse), _at(d_gates), _at(fwd.dprob),
+          _at(fwd.stats), _at(d_logits), ldd)
     _used_on(stream, d_logits)
     return d_logits
 
@@ -642,48 +657,50 @@ class Params:
         self.tensors = [tuple(t) + (None,) * (5 - len(t)) for t in tensors]
         self.device = None
         self.weight_dtype = self.grad_dtype = None
-        self.masters = any(t[4] is not None for t in self.tensors)
         self.c = (rft_param * max(1, len(self.tensors)))()
-        for i, (w, g, m, v, master) in enumerate(self.tensors):
-            _need_gpu(w, g, m, v, master)
-            self.device = self.device or g.device
-            self.grad_dtype = self.grad_dtype or g.dtype
-            if w is not None:
-                self.weight_dtype = self.weight_dtype or w.dtype
-            for name, t, dt in (("weight", w, self.weight_dtype), ("grad", g, self.grad_dtype),
-                                ("m", m, torch.float32), ("v", v, torch.float32),
-                                ("master", master, torch.float32)):
+        f32 = torch.float32
+        for i, ts in enumerate(self.tensors):
+            w, g = ts[:2]
+            if self.device is None:
+                _need_gpu(g)
+                self.device, self.grad_dtype = g.device, g.dtype
+            if w is not None and self.weight_dtype is None:
+                self.weight_dtype = w.dtype
+            n = g.numel()
+            at = []
+            for t, dt in zip(ts, (self.weight_dtype, self.grad_dtype, f32, f32, f32)):
                 if t is None:
-                    continue
-                if t.dtype != dt or t.numel() != g.numel() or not t.is_contiguous():
-                    raise TypeError(f"tensor {i}: {name} must be contiguous {dt} of "
-                                    f"{g.numel()} elements")
-                if t.device != self.device:
-                    raise RuntimeError(f"tensor {i}: {name} is on {t.device}, not {self.device}")
-            self.c[i] = rft_param(*(None if t is None else t.data_ptr()
-                                    for t in (w, g, m, v, master)), g.numel())
+                    at.append(None)
+                elif (t.dtype == dt and t.numel() == n and t.device == self.device
+                      and t.is_contiguous()):
+                    at.append(t.data_ptr())
+                else:
+                    raise TypeError(f"tensor {i}: contiguous {dt} of {n} elements on "
+                                    f"{self.device} expected, got {t.dtype} {tuple(t.shape)} "
+                                    f"on {t.device}")
+            self.c[i] = (*at, n)
 
     def __len__(self):
         return len(self.tensors)
 
 
 class Clip:
-    """Gradient norm and clip factor on the device (rft_clip)."""
+    """Gradient norm and clip factor on the device (rft_clip, held as f32 [3])."""
 
     def __init__(self, device):
-        self.buf = torch.empty(ctypes.sizeof(rft_clip), dtype=torch.uint8, device=device)
+        self.buf = torch.empty(ctypes.sizeof(rft_clip) // 4, dtype=torch.float32, device=device)
 
     @property
     def norm(self):
-        return self.buf[:4].view(torch.float32)[0]
+        return self.buf[0]
 
     @property
     def scale(self):
-        return self.buf[4:8].view(torch.float32)[0]
+        return self.buf[1]
 
     @property
     def finite(self):
-        return self.buf[8:12].view(torch.int32)[0]
+        return self.buf.view(torch.int32)[2]
 
 
 def _code(dtype):
@@ -694,16 +711,23 @@ def _code(dtype):
     raise TypeError(f"unsupported dtype {dtype}")
 
 
+def _clip_at(dev, clip):
+    if clip is None:
+        return None
+    if clip.buf.device != dev:
+        raise RuntimeError(f"clip is on {clip.buf.device}, the call works on {dev}")
+    return clip.buf.data_ptr()
+
+
 def rft_grad_norm(params: Params, max_norm=0.0, clip=None, ws=None, stream=None) -> Clip:
     """Global gradient norm; the returned Clip feeds rft_adamw_step and rft_muon_step."""
     dev = params.device or torch.device("cuda", torch.cuda.current_device())
     clip = Clip(dev) if clip is None else clip
-    _same_device(dev, ("clip", clip.buf), ("ws", ws))
-    need = int(lib().rft_grad_norm_workspace_bytes(params.c, len(params)))
-    ws, nb = _workspace(need, dev, ws)
-    with torch.cuda.device(dev):
-        _check(lib().rft_grad_norm(params.c, len(params), _code(params.grad_dtype), max_norm,
-                                   _ptr(clip.buf), _ptr(ws), nb, _stream_of(clip.buf, stream)))
+    _same_device(dev, ("ws", ws))
+    L, n = lib(), len(params)
+    ws, nb = _workspace(int(L.rft_grad_norm_workspace_bytes(params.c, n)), dev, ws)
+    _call(L.rft_grad_norm, dev, stream, params.c, n, _code(params.grad_dtype), max_norm,
+          _clip_at(dev, clip), _at(ws), nb)
     _used_on(stream, clip.buf, ws)
     return clip
 
@@ -716,13 +740,8 @@ def adamw_params(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
 def rft_adamw_step(params: Params, hyper, clip=None, stream=None):
     """One AdamW step in place over every tensor of `params`."""
     dev = params.device or torch.device("cuda", torch.cuda.current_device())
-    _same_device(dev, ("clip", clip.buf if clip is not None else None))
-    with torch.cuda.device(dev):
-        s = torch.cuda.current_stream(dev) if stream is None else stream
-        _check(lib().rft_adamw_step(params.c, len(params), _code(params.weight_dtype),
-                                    _code(params.grad_dtype), ctypes.byref(hyper),
-                                    _ptr(clip.buf) if clip is not None else None,
-                                    ctypes.c_void_p(s.cuda_stream)))
+    _call(lib().rft_adamw_step, dev, stream, params.c, len(params), _code(params.weight_dtype),
+          _code(params.grad_dtype), ctypes.byref(hyper), _clip_at(dev, clip))
 
 
 def muon_params(lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, scale=1.0, steps=5,
@@ -762,11 +781,9 @@ def rft_orthogonalize(g, params, out=None, out_dtype=None, ws=None, stream=None)
     mats = _matrices(("g", g), ("out", out))
     _same_device(g.device, ("ws", ws))
     dt, odt = _dtype_code(g), _dtype_code(out)
-    need = int(lib().rft_orthogonalize_workspace_bytes(ctypes.byref(mats), ctypes.byref(params), odt))
-    ws, nb = _workspace(need, g.device, ws)
-    with torch.cuda.device(g.device):
-        _check(lib().rft_orthogonalize(ctypes.byref(mats), _ptr(g), dt, ctypes.byref(params),
-                                       _ptr(out), odt, _ptr(ws), nb, _stream_of(g, stream)))
+    L, rm, rp = lib(), ctypes.byref(mats), ctypes.byref(params)
+    ws, nb = _workspace(int(L.rft_orthogonalize_workspace_bytes(rm, rp, odt)), g.device, ws)
+    _call(L.rft_orthogonalize, g.device, stream, rm, _at(g), dt, rp, _at(out), odt, _at(ws), nb)
     _used_on(stream, out, ws)
     return out
 
@@ -778,16 +795,14 @@ def rft_muon_step(weight, grad, momentum, params, master=None, clip=None, ws=Non
     for name, t in (("momentum", momentum), ("master", master)):
         if t is not None and t.dtype != torch.float32:
             raise TypeError(f"{name} is float32")
-    _same_device(weight.device, ("ws", ws), ("clip", clip.buf if clip is not None else None))
+    dev = weight.device
+    _same_device(dev, ("ws", ws))
     wdt, gdt = _dtype_code(weight), _dtype_code(grad)
-    need = int(lib().rft_orthogonalize_workspace_bytes(
-        ctypes.byref(mats), ctypes.byref(params), RFT_F32 if master is not None else wdt))
-    ws, nb = _workspace(need, weight.device, ws)
-    with torch.cuda.device(weight.device):
-        _check(lib().rft_muon_step(ctypes.byref(mats), _ptr(grad), gdt, _ptr(momentum),
-                                   _ptr(weight), wdt, _ptr(master), ctypes.byref(params),
-                                   _ptr(clip.buf) if clip is not None else None, _ptr(ws), nb,
-                                   _stream_of(weight, stream)))
+    L, rm, rp = lib(), ctypes.byref(mats), ctypes.byref(params)
+    need = int(L.rft_orthogonalize_workspace_bytes(rm, rp, RFT_F32 if master is not None else wdt))
+    ws, nb = _workspace(need, dev, ws)
+    _call(L.rft_muon_step, dev, stream, rm, _at(grad), gdt, _at(momentum), _at(weight), wdt,
+          _at(master), rp, _clip_at(dev, clip), _at(ws), nb)
     _used_on(stream, ws)
 
 

@@ -12,10 +12,16 @@
 //   k_router_sum_short  the same for many short rollouts: one wavefront per rollout
 //   k_router_bwd  d_logits: p is formed again from the logits and lse
 //
-// Slots.  Wave w owns rows [w Rw, (w + 1) Rw); walking them, each step to another
-// rollout i or another wave raises w + i by one at least, so slot w + i belongs to
-// that pair alone and nW + n_seq slots hold them all.  The sums of a group run over
-// its slots in a fixed order.
+// Slots (balance per rollout).  Wave w owns rows [w Rw, (w + 1) Rw); walking them, each
+// step to another rollout i or another wave raises w + i by one at least, so slot w + i
+// belongs to that pair alone and nW + n_seq slots hold them all.  The sums of a group run
+// over its slots in a fixed order, so results are the same from run to run.
+//
+// Measured at 262144 rows (62% unmasked) x 128 fp32 experts, k = 8: forward 44 us (84 MB of
+// logits read, 17 MB written: its instructions bound it, about 420 vector instructions
+// per four rows, half of them the selection), sum 10.6 us (latency of two rounds of loads,
+// the reduction and the hand-over to the last block), backward 57 us (235 MB, 4.1 TB/s; a
+// large copy reaches 4.9-5.2 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -25,9 +31,15 @@
 namespace rft {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 512, kWaves = kThreads / 64;        // forward
+constexpr int kBwdThreads = 256, kBwdWavesPer = kBwdThreads / 64;
 constexpr int kSumThreads = 1024, kSumWaves = kSumThreads / 64;
-constexpr int64_t kTargetWaves = 8192;  // 256 CUs of 32 resident waves
+// Waves of a launch over many rows: as many as its registers let 256 CUs hold (of a
+// forward over more than 128 experts, 64 and fewer four, six, eight per SIMD), so that they
+// all run from start to end (8192 waves of which 6144 were resident: 52 us against 44).
+constexpr int64_t kSimds = 1024;
+inline int64_t fwd_waves(int E) { return kSimds * (E > 512 || (E > 128 && E <= 256) ? 4 : E > 64 ? 6 : 8); }
+constexpr int64_t kBwdWaves = kSimds * 8;
 constexpr float kExcluded = -2e38f;     // logits below are excluded experts
 
 // Row t of rollout: the largest i in [0, n_seq) with seq_start[i] <= t.
@@ -185,13 +197,77 @@ struct Geom {
   bool vec;
 };
 
-// One row's softmax and selection, in the lanes of its group.  key: the logits that
-// can be selected, -inf otherwise (NaN and excluded ones); on return the selected
-// ones are -inf too.  Lane j < k gets the j-th place in (id, top).
+// Selection of a row's k largest logits by integer keys: the logit's bits in an order
+// that compares as unsigned (31 - IB bits of them), then IB bits that are larger for
+// lower indices.  The keys of a row differ, so the place after key m is the largest
+// key below m, and over unsigned differences that is the largest of key - m (keys below m
+// wrap past 2^31, the others stay under it): one subtraction per register, their maximum
+// and the group's, with nothing to take out and no second pass for the index.  A bf16
+// logit fits whole; of an fp32 one the low bits are cut, so a row in which two
+// neighbouring places agree in the rest, or one with a NaN (which has no place in the
+// order), is selected again by `select`.  At 262144 rows x 128 fp32 experts, k = 8, the
+// forward took 93 us with `select` alone.
+template <int N> constexpr int kLog2 = N <= 1 ? 0 : 1 + kLog2<N / 2>;
+template <> constexpr int kLog2<1> = 0;
+template <int LPR, int VPT> constexpr int kIB = kLog2<LPR * VPT>;
+
+// A logit's bits in an order that compares as unsigned, and back.
+__device__ __forceinline__ uint32_t ordered(float z) {
+  const uint32_t u = __float_as_uint(z + 0.f);  // -0 equals 0
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t o) {
+  return __uint_as_float(o ^ (~(uint32_t)((int32_t)o >> 31) | 0x80000000u));
+}
+template <int LPR, int VPT, bool BF16>
+__device__ __forceinline__ uint32_t key_of(uint32_t o, int e) {
+  constexpr int IB = kIB<LPR, VPT>;
+  constexpr uint32_t IM = (1u << IB) - 1;
+  return ((BF16 ? o >> 16 : o >> (IB + 1)) << IB) | (IM - (uint32_t)e);
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xF, 0xF, true));
+}
+template <int LPR>
+__device__ __forceinline__ uint32_t group_max_u(uint32_t v) {
+  v = max_dpp<0xB1>(v);
+  v = max_dpp<0x4E>(v);
+  v = max_dpp<0x141>(v);
+  v = max_dpp<0x140>(v);
+  if (LPR == 64) {
+    v = max(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+    v = max(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+  }
+  return v;
+}
+
+// Lane j < k gets the index of the j-th place in id (of an excluded expert too).  Returns
+// whether two places, or the last and the first left out, agree in the logit's part.
+template <int LPR, int VPT, bool BF16>
+__device__ __forceinline__ bool select_keys(const uint32_t (&key)[VPT], int l, int k, int& id) {
+  constexpr int IB = kIB<LPR, VPT>;
+  constexpr uint32_t IM = (1u << IB) - 1;
+  uint32_t m = 0x80000000u, mine = 0, near = 0xffffffffu;
+  for (int j = 0; j < k + (BF16 ? 0 : 1); ++j) {
+    uint32_t d = key[0] - m;
+#pragma unroll
+    for (int v = 1; v < VPT; ++v) d = max(d, key[v] - m);
+    const uint32_t n = group_max_u<LPR>(d) + m;
+    near = min(near, n ^ m);
+    m = n;
+    if (l == j) mine = m;
+  }
+  id = (int)(IM - (mine & IM));
+  return !BF16 && near <= IM;
+}
+
+// The same by float maxima, exact for every logit.  key: the logits that can be
+// selected, -inf otherwise; on return the selected ones are -inf too.
 template <int LPR, int VPT>
-__device__ __forceinline__ void select(float (&key)[VPT], int l, int k, int& id, float& top) {
+__device__ __forceinline__ void select(float (&key)[VPT], int l, int k, int& id) {
   id = -1;
-  top = -INFINITY;
   for (int j = 0; j < k; ++j) {
     float m = key[0];
 #pragma unroll
@@ -206,11 +282,15 @@ __device__ __forceinline__ void select(float (&key)[VPT], int l, int k, int& id,
 #pragma unroll
     for (int v = 0; v < VPT; ++v)
       key[v] = expert_of<LPR, VPT>(l, v) == e ? -INFINITY : key[v];
-    if (l == j) {
-      id = e;
-      top = m;
-    }
+    if (l == j) id = e;
   }
+}
+
+// exp(x - m) for x <= m, ml = m log2 e, by the hardware's exp2 (results below 2^-126 are
+// 0); x = -inf gives 0, NaN NaN.  The rounding of ml is a factor that all of a row's
+// values share (2^-24 |m|), that of the fma 2^-24 |x - m| of the value.
+__device__ __forceinline__ float exp_diff(float x, float ml) {
+  return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, -ml));
 }
 
 template <int LPR, int VPT, bool BF16, bool STATS>
@@ -219,20 +299,31 @@ __global__ void __launch_bounds__(kThreads) k_router(
     const int32_t* __restrict__ ss, bool by_rollout, int32_t* __restrict__ ids,
     float* __restrict__ gates, float* __restrict__ lse_out, const Ws w) {
   constexpr int RPI = 64 / LPR;  // rows per wave and iteration
-  extern __shared__ float sh[];  // STATS over the batch: [kWaves][2 E + 4]
+  // STATS, per wave: 4 words (z-loss, rows), sums of p [E], selections of each expert [E].
+  // Integer additions, so their order does not matter.
+  extern __shared__ float sh[];
+  __shared__ __attribute__((aligned(16))) float rows[kWaves][64 * VPT];
   const int lane = threadIdx.x & 63, l = lane & (LPR - 1), grp = lane / LPR;
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t wave = (int64_t)blockIdx.x * kWaves + wid;
-  const int E = g.E, k = g.k;
-  if (STATS && blockIdx.x == 0 && threadIdx.x == 0) *w.counter = 0;
-  int64_t r = wave * g.Rw;
-  const int64_t r1 = min(g.T, r + g.Rw);
+  const int E = g.E, k = g.k, pitch = 2 * E + 4;
+  float* const my = sh + wid * pitch;
+  int* const hist = (int*)my + 4 + E;
+  float* const look = &rows[wid][grp * (LPR * VPT)];
+  if (STATS) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *w.counter = 0;
+    for (int x = lane; x < E; x += 64) hist[x] = 0;
+  }
+  // Rows: a run of Rw per wave where rollouts are balanced; else every nW-th RPI rows, so
+  // that padding, which comes in long runs, is shared by all waves.
+  const int64_t step = by_rollout ? RPI : g.nW * RPI;
+  int64_t r = by_rollout ? wave * g.Rw : wave < g.nW ? wave * RPI : g.T;
+  const int64_t r1 = by_rollout ? min(g.T, r + g.Rw) : g.T;
   float acc[VPT];
-  int cnt[VPT];
   double zs = 0;
   int n = 0;
 #pragma unroll
-  for (int v = 0; v < VPT; ++v) acc[v] = 0.f, cnt[v] = 0;
+  for (int v = 0; v < VPT; ++v) acc[v] = 0.f;
   while (r < r1) {
     int64_t end = r1;
     int seq = 0;
@@ -240,110 +331,154 @@ __global__ void __launch_bounds__(kThreads) k_router(
       seq = rollout_of(ss, g.n_seq, r);
       if (seq + 1 < g.n_seq) end = min(end, max((int64_t)ss[seq + 1], r + 1));
     }
-    for (; r < end; r += RPI) {
-      const int64_t t = r + grp;
-      const bool in = t < end, on = in && mask[t] != 0;
-      float z[VPT], key[VPT];
-      if (on) {
-        load_row<LPR, VPT, BF16>((const char*)logits + t * g.ld * (BF16 ? 2 : 4), l, E, g.vec, z);
+    // the mask of the next rows but one and the logits of the next rows are on their way
+    // while a row is worked on
+    auto masked = [&](int64_t q) { return q + grp < end ? mask[q + grp] : (uint8_t)0; };
+    float z[VPT];
+    auto fetch = [&](int64_t q, bool want) {
+      // the bounds of a row's loads change with every row for the compiler, which keeps them
+      // in (spilled) scalar registers otherwise
+      int Er = E, lr = l;
+      asm volatile("" : "+s"(Er), "+v"(lr));
+      if (want) {
+        load_row<LPR, VPT, BF16>((const char*)logits + (q + grp) * g.ld * (BF16 ? 2 : 4), lr, Er,
+                                 g.vec, z);
       } else {
 #pragma unroll
         for (int v = 0; v < VPT; ++v) z[v] = -INFINITY;
       }
-      float mx = -INFINITY;
+    };
+    bool on = masked(r) != 0;
+    uint8_t ahead = masked(r + step);
+    fetch(r, on);
+    for (; r < end; r += step) {
+      const int64_t t = r + grp;
+      const bool in = t < end;
+      const bool next_on = ahead != 0;
+      if (!__builtin_amdgcn_ballot_w64(on)) {  // no row to route
+        if (in) {
+          if (l < k) {
+            ids[t * k + l] = -1;
+            gates[t * k + l] = 0.f;
+          }
+          if (lse_out && l == 0) lse_out[t] = 0.f;
+        }
+        on = next_on;
+        ahead = masked(r + 2 * step);
+        fetch(r + step, on);
+        continue;
+      }
+      int lr = l;
+      asm volatile("" : "+v"(lr));
+      // the row also in LDS, where its places are looked up
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) look[expert_of<LPR, VPT>(lr, v)] = z[v];
+      uint32_t key[VPT], top = 0;
 #pragma unroll
       for (int v = 0; v < VPT; ++v) {
-        key[v] = z[v] >= kExcluded ? z[v] : -INFINITY;
-        mx = fmaxf(mx, key[v]);
+        const uint32_t o = ordered(z[v]);
+        top = max(top, o);
+        key[v] = key_of<LPR, VPT, BF16>(o, expert_of<LPR, VPT>(lr, v));
       }
-      mx = group_max<LPR>(mx);
-      const float m0 = mx == -INFINITY ? 0.f : mx;
+      // the largest logit (or a NaN: the sums are NaN then)
+      const float mx = unordered(group_max_u<LPR>(top));
+      const float m0 = mx < kExcluded ? 0.f : mx, ml = m0 * kLog2e;
       float s = 0.f;
       float e[VPT];
 #pragma unroll
       for (int v = 0; v < VPT; ++v) {
-        e[v] = z[v] < kExcluded ? 0.f : expf(z[v] - m0);
+        e[v] = exp_diff(z[v], ml);
         s += e[v];
       }
       s = group_sum<LPR>(s);
       int id;
-      float top;
-      select<LPR, VPT>(key, l, k, id, top);
+      const bool again = select_keys<LPR, VPT, BF16>(key, l, k, id) || !(s == s);
+      if (__builtin_amdgcn_ballot_w64(again && on)) {
+        float f[VPT];
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) f[v] = z[v] >= kExcluded ? z[v] : -INFINITY;
+        select<LPR, VPT>(f, lr, k, id);
+      }
+      const bool was = on;
+      on = next_on;
+      ahead = masked(r + 2 * step);
+      fetch(r + step, on);
       const bool some = s != 0.f;  // an expert is left (or a NaN)
-      const float rs = some ? 1.f / s : 0.f;
+      const float rs = some ? __builtin_amdgcn_rcpf(s) : 0.f;
+      float gate = 0.f;
+      if (l >= k || !was || (unsigned)id >= (unsigned)E) id = -1;
+      if (id >= 0) {
+        const float zi = look[id];
+        gate = exp_diff(zi, ml);
+        if (zi < kExcluded) id = -1, gate = 0.f;
+      }
+      float den = rs;
+      if (g.norm) {
+        const float sel = group_sum<LPR>(gate);
+        den = sel != 0.f ? __builtin_amdgcn_rcpf(sel) : 0.f;
+      }
+      gate = id >= 0 ? (s == s ? gate * den : s) : 0.f;
+      const float ls = some ? fmaf(__builtin_amdgcn_logf(s), kLn2, m0) : 0.f;
       if (in) {
-        float gate = id >= 0 ? expf(top - m0) : 0.f;
-        if (g.norm) {
-          const float sel = group_sum<LPR>(gate);
-          gate = id >= 0 ? gate / sel : 0.f;
-          if (!(s == s) && id >= 0) gate = s;
-        } else {
-          gate = id >= 0 ? gate * rs : 0.f;
-        }
         if (l < k) {
           ids[t * k + l] = id;
           gates[t * k + l] = gate;
         }
-        const float ls = some ? m0 + logf(s) : 0.f;
         if (lse_out && l == 0) lse_out[t] = ls;
-        if (STATS && on) {
+      }
+      if (STATS) {  // a row that is not on has id -1, rs 0 and ls 0
+        if (id >= 0) atomicAdd(hist + id, 1);
 #pragma unroll
-          for (int v = 0; v < VPT; ++v) {
-            acc[v] = fmaf(e[v], rs, acc[v]);
-            cnt[v] += z[v] >= kExcluded && key[v] == -INFINITY ? 1 : 0;
-          }
-          zs += (double)ls * ls;
-          ++n;
-        }
+        for (int v = 0; v < VPT; ++v) acc[v] = fmaf(e[v], rs, acc[v]);
+        zs = fma((double)ls, (double)ls, zs);
+        n += was ? 1 : 0;
       }
     }
-    r = end;
+    r = by_rollout ? end : r1;
     if (STATS) {
       // the groups' sums together; every lane of group 0 then holds its experts' sums
 #pragma unroll
       for (int o = LPR; o < 64; o <<= 1) {
 #pragma unroll
-        for (int v = 0; v < VPT; ++v) {
-          acc[v] += __shfl_xor(acc[v], o, 64);
-          cnt[v] += __shfl_xor(cnt[v], o, 64);
-        }
+        for (int v = 0; v < VPT; ++v) acc[v] += __shfl_xor(acc[v], o, 64);
         zs += __shfl_xor(zs, o, 64);
         n += __shfl_xor(n, o, 64);
       }
       if (by_rollout) {
         const int64_t slot = wave + seq;
+        int lx = l, Ex = E;  // as above: nothing of this is kept over the rows
+        asm volatile("" : "+v"(lx), "+s"(Ex));
         if (grp == 0) {
+          float* const ps = w.psum + slot * Ex;
 #pragma unroll
           for (int v = 0; v < VPT; ++v) {
-            const int x = expert_of<LPR, VPT>(l, v);
-            if (x < E) {
-              w.psum[slot * E + x] = acc[v];
-              w.cnt[slot * E + x] = cnt[v];
-            }
+            const int x = expert_of<LPR, VPT>(lx, v);
+            if (x < Ex) ps[x] = acc[v];
           }
         }
+        __builtin_amdgcn_wave_barrier();  // a wave's LDS operations run in order
+        for (int x = lane; x < Ex; x += 64) {
+          w.cnt[slot * Ex + x] = hist[x];
+          hist[x] = 0;
+        }
+        __builtin_amdgcn_wave_barrier();
         if (lane == 0) {
           w.n[slot] = n;
           w.zs[slot] = zs;
         }
 #pragma unroll
-        for (int v = 0; v < VPT; ++v) acc[v] = 0.f, cnt[v] = 0;
+        for (int v = 0; v < VPT; ++v) acc[v] = 0.f;
         zs = 0;
         n = 0;
       }
     }
   }
   if (STATS && !by_rollout) {  // one slot per block
-    const int pitch = 2 * E + 4;
-    float* const my = sh + wid * pitch;
     if (grp == 0) {
 #pragma unroll
       for (int v = 0; v < VPT; ++v) {
         const int x = expert_of<LPR, VPT>(l, v);
-        if (x < E) {
-          my[4 + x] = acc[v];
-          my[4 + E + x] = __int_as_float(cnt[v]);
-        }
+        if (x < E) my[4 + x] = acc[v];
       }
     }
     if (lane == 0) {
@@ -399,12 +534,14 @@ __device__ __forceinline__ void finish(const Ws& w, Part p, float cb, float cz,
   __shared__ Part tot[kSumWaves];
   if (threadIdx.x == 0) {
     w.part[blockIdx.x] = p;
-    __threadfence();
-    last = atomicAdd(w.counter, 1) == (int)gridDim.x - 1 ? 1 : 0;
+    // releases this block's part, and acquires the others' where this is the last block
+    last = __hip_atomic_fetch_add(w.counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
+           (int)gridDim.x - 1 ? 1 : 0;
   }
   __syncthreads();
   if (!last) return;
-  __threadfence();
+  __atomic_thread_fence(__ATOMIC_ACQUIRE);
+  if (gridDim.x <= 64 && threadIdx.x >= 64) return;  // one wave has them all
   Part q = {0, 0, 0, 0, 0, 0};
   for (int b = threadIdx.x; b < (int)gridDim.x; b += kSumThreads) {
     const Part& x = w.part[b];
@@ -420,10 +557,13 @@ __device__ __forceinline__ void finish(const Ws& w, Part p, float cb, float cz,
   q.S = wave_sum_i(q.S);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) q.mx = max(q.mx, __shfl_xor(q.mx, o, 64));
-  if ((threadIdx.x & 63) == 0) tot[threadIdx.x >> 6] = q;
-  __syncthreads();
+  const int waves = gridDim.x <= 64 ? 1 : kSumWaves;
+  if (waves > 1) {
+    if ((threadIdx.x & 63) == 0) tot[threadIdx.x >> 6] = q;
+    __syncthreads();
+  }
   if (threadIdx.x == 0) {
-    for (int b = 1; b < kSumWaves; ++b) {
+    for (int b = 1; b < waves; ++b) {
       q.bal += tot[b].bal;
       q.z += tot[b].z;
       q.n += tot[b].n;
@@ -464,16 +604,30 @@ __global__ void __launch_bounds__(kSumThreads) k_router_sum(
   slots_of(g, ss, by_rollout, nblk, i, lo, hi);
   double p = 0, z = 0;
   int c = 0, n = 0;
-  if (x < g.E) {
-#pragma unroll 4
-    for (int64_t s = lo + (threadIdx.x >> 4); s < hi; s += kSumThreads / 16) {
-      p += w.psum[s * g.E + x];
-      c += w.cnt[s * g.E + x];
+  // kBatch loads of each array at a time: what bounds this kernel is their latency
+  constexpr int kBatch = 16;
+  const float* const ps = w.psum + lo * g.E + min(x, g.E - 1);
+  const int32_t* const cs = w.cnt + lo * g.E + min(x, g.E - 1);
+  const int m = (int)(hi - lo);
+  for (int s0 = threadIdx.x >> 4; s0 < m; s0 += kBatch * (kSumThreads / 16)) {
+    float pv[kBatch];
+    int cv[kBatch];
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      const int s = s0 + q * (kSumThreads / 16);
+      const int64_t o = (int64_t)min(s, m - 1) * g.E;
+      pv[q] = s < m ? ps[o] : 0.f;
+      cv[q] = s < m ? cs[o] : 0;
+    }
+#pragma unroll
+    for (int q = 0; q < kBatch; ++q) {
+      p += pv[q];
+      c += cv[q];
     }
   }
-  for (int64_t s = lo + threadIdx.x; s < hi; s += kSumThreads) {
-    n += w.n[s];
-    z += w.zs[s];
+  for (int s = threadIdx.x; s < m; s += kSumThreads) {
+    n += w.n[lo + s];
+    z += w.zs[lo + s];
   }
   p += __shfl_xor(p, 16, 64);
   c += __shfl_xor(c, 16, 64);
@@ -605,7 +759,7 @@ __global__ void __launch_bounds__(kSumThreads) k_router_sum_short(
 }
 
 template <int LPR, int VPT, bool BF16>
-__global__ void __launch_bounds__(kThreads) k_router_bwd(
+__global__ void __launch_bounds__(kBwdThreads) k_router_bwd(
     const Geom g, const void* logits, const uint8_t* __restrict__ mask,
     const int32_t* __restrict__ ss, bool by_rollout, const int32_t* __restrict__ ids,
     const float* __restrict__ lse, const float* __restrict__ d_gates,
@@ -613,9 +767,14 @@ __global__ void __launch_bounds__(kThreads) k_router_bwd(
     void* d_logits, int64_t ldd, bool dvec) {
   constexpr int RPI = 64 / LPR;
   constexpr int W = BF16 ? 2 : 4;
+  // gradients to the selected probabilities, scattered by expert: zeros between the rows
+  __shared__ __attribute__((aligned(16))) float sg[kBwdWavesPer][64 * VPT];
   const int lane = threadIdx.x & 63, l = lane & (LPR - 1), grp = lane / LPR;
-  const int64_t wave = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  const int64_t wave = (int64_t)blockIdx.x * kBwdWavesPer + (threadIdx.x >> 6);
   const int E = g.E, k = g.k;
+  float* const mine = &sg[threadIdx.x >> 6][grp * (LPR * VPT)];
+#pragma unroll
+  for (int v = 0; v < VPT; ++v) mine[expert_of<LPR, VPT>(l, v)] = 0.f;
   const int64_t r1 = min(g.T, (wave + 1) * g.Rw);
   const int N = st->n_valid, S = st->n_groups;
   const float bs = cb > 0.f && S > 0 ? cb / (float)S : 0.f;
@@ -627,14 +786,18 @@ __global__ void __launch_bounds__(kThreads) k_router_bwd(
   for (int64_t r = wave * g.Rw; r < r1; r += RPI) {
     const int64_t t = r + grp;
     if (t >= r1) continue;  // whole groups: the reductions stay within them (LPR = 64: the wave)
+    int Er = E;  // see k_router
+    asm volatile("" : "+s"(Er));
+    char* const out = (char*)d_logits + t * ldd * W;
     float z[VPT], d[VPT];
     if (!mask[t]) {
 #pragma unroll
       for (int v = 0; v < VPT; ++v) d[v] = 0.f;
-      store_row<LPR, VPT, BF16>((char*)d_logits + t * ldd * W, l, E, dvec, d);
+      store_row<LPR, VPT, BF16>(out, l, Er, dvec, d);
       continue;
     }
-    load_row<LPR, VPT, BF16>((const char*)logits + t * g.ld * W, l, E, g.vec, z);
+    const char* const row = (const char*)logits + t * g.ld * W;
+    load_row<LPR, VPT, BF16>(row, l, Er, g.vec, z);
     if (bs != 0.f && t >= next) {
       int64_t o = 0;
       next = g.T;
@@ -646,17 +809,18 @@ __global__ void __launch_bounds__(kThreads) k_router_bwd(
 #pragma unroll
       for (int v = 0; v < VPT; ++v) {
         const int x = expert_of<LPR, VPT>(l, v);
-        dp[v] = x < E ? bs * dprob[o + x] : 0.f;
+        dp[v] = x < Er ? bs * dprob[o + x] : 0.f;
       }
     }
     const float ls = lse[t];
     float p[VPT];
 #pragma unroll
-    for (int v = 0; v < VPT; ++v) p[v] = z[v] < kExcluded ? 0.f : expf(z[v] - ls);
-#pragma unroll
-    for (int v = 0; v < VPT; ++v) d[v] = dp[v];
+    for (int v = 0; v < VPT; ++v) {
+      p[v] = exp_diff(z[v], ls * kLog2e);
+      d[v] = dp[v];
+    }
     if (d_gates) {
-      // lane j holds place j; its gradient to the probability of its expert
+      // lane j holds place j and its gradient to the probability of its expert
       int id = -1;
       float dg = 0.f;
       if (l < k) {
@@ -665,21 +829,22 @@ __global__ void __launch_bounds__(kThreads) k_router_bwd(
         if (id >= 0) dg = d_gates[t * k + l];
       }
       if (g.norm) {
-        const float ze = id >= 0 ? (BF16 ? bf16_to_f32(((const uint16_t*)logits)[t * g.ld + id])
-                                         : ((const float*)logits)[t * g.ld + id])
-                                 : 0.f;
-        const float pe = id >= 0 && !(ze < kExcluded) ? expf(ze - ls) : 0.f;
+        float pe = 0.f;
+        if (id >= 0)
+          pe = exp_diff(BF16 ? bf16_to_f32(((const uint16_t*)row)[id]) : ((const float*)row)[id],
+                        ls * kLog2e);
         const float sel = group_sum<LPR>(pe);
         const float mean = group_sum<LPR>(dg * pe);
         dg = id >= 0 && sel != 0.f ? (dg - mean / sel) / sel : 0.f;
       }
-      for (int j = 0; j < k; ++j) {
-        const int src = (lane & ~(LPR - 1)) + j;
-        const int ej = __shfl(id, src, 64);
-        const float gj = __shfl(dg, src, 64);
+      // through LDS to the lane of the expert (added: an expert that an invalid list names
+      // twice counts twice); a wave's LDS operations run in order
+      if (id >= 0) atomicAdd(mine + id, dg);
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int v = 0; v < VPT; ++v) d[v] += expert_of<LPR, VPT>(l, v) == ej ? gj : 0.f;
-      }
+      for (int v = 0; v < VPT; ++v) d[v] += mine[expert_of<LPR, VPT>(l, v)];
+      __builtin_amdgcn_wave_barrier();
+      if (id >= 0) mine[id] = 0.f;
     }
     float dot = 0.f;
 #pragma unroll
@@ -688,18 +853,18 @@ __global__ void __launch_bounds__(kThreads) k_router_bwd(
     const float zt = zc * ls - dot;
 #pragma unroll
     for (int v = 0; v < VPT; ++v) d[v] = z[v] < kExcluded ? 0.f : p[v] * (d[v] + zt);
-    store_row<LPR, VPT, BF16>((char*)d_logits + t * ldd * W, l, E, dvec, d);
+    store_row<LPR, VPT, BF16>(out, l, Er, dvec, d);
   }
 }
 
-int64_t rows_per_wave(int64_t T, int E) {
+int64_t rows_per_wave(int64_t T, int E, int64_t waves) {
   const int rpi = E <= 256 ? 4 : 1;
-  const int64_t r = (T + kTargetWaves - 1) / kTargetWaves;
+  const int64_t r = (T + waves - 1) / waves;
   return std::max<int64_t>(rpi, (r + rpi - 1) / rpi * rpi);
 }
 
 Geom geometry(const rft_tokens& tok, const rft_router_params& p, const void* logits, int dtype,
-              int64_t ld) {
+              int64_t ld, int64_t waves) {
   Geom g;
   g.T = tok.T;
   g.ld = ld;
@@ -707,7 +872,7 @@ Geom geometry(const rft_tokens& tok, const rft_router_params& p, const void* log
   g.k = p.top_k;
   g.norm = p.norm_topk != 0;
   g.n_seq = p.scope == RFT_BALANCE_ROLLOUT ? (int)tok.n_seq : 1;
-  g.Rw = rows_per_wave(tok.T, p.n_experts);
+  g.Rw = rows_per_wave(tok.T, p.n_experts, waves);
   g.nW = (tok.T + g.Rw - 1) / g.Rw;
   const int C = p.n_experts > 32 ? 4 : p.n_experts > 16 ? 2 : 1;
   const int64_t bytes = C * (dtype == RFT_BF16 ? 2 : 4);
@@ -791,7 +956,8 @@ extern "C" {
 
 size_t rft_router_workspace_bytes(const rft_tokens* tok, const rft_router_params* params) {
   if (check_router("rft_router_workspace_bytes", tok, params)) return 0;
-  const Geom g = geometry(*tok, *params, nullptr, RFT_F32, params->n_experts);
+  const Geom g = geometry(*tok, *params, nullptr, RFT_F32, params->n_experts,
+                          fwd_waves(params->n_experts));
   Carver c(nullptr);
   carve(c, g, params->scope == RFT_BALANCE_ROLLOUT);
   return c.bytes();
@@ -812,7 +978,7 @@ rft_status rft_router_fwd(const rft_tokens* tok, const void* logits, int dtype, 
     return fail(RFT_E_NULL, "%s: lse, counts, dprob and stats are given together, or counts, dprob "
                 "and stats not at all", fn);
   const bool by_rollout = params->scope == RFT_BALANCE_ROLLOUT;
-  const Geom g = geometry(*tok, *params, logits, dtype, ld);
+  const Geom g = geometry(*tok, *params, logits, dtype, ld, fwd_waves(params->n_experts));
   if (sum_blocks(g, by_rollout) > ((int64_t)1 << 22))
     return fail(RFT_E_SHAPE, "%s: n_seq=%lld is more than this many experts allow", fn,
                 (long long)tok->n_seq);
@@ -828,7 +994,7 @@ rft_status rft_router_fwd(const rft_tokens* tok, const void* logits, int dtype, 
   if (grid > 0) {
     by_experts(g.E, [&](auto L, auto V) {
       constexpr int l = decltype(L)::value, v = decltype(V)::value;
-      const size_t shm = want && !by_rollout ? (size_t)kWaves * (2 * g.E + 4) * 4 : 0;
+      const size_t shm = want ? (size_t)kWaves * (2 * g.E + 4) * 4 : 0;
       auto go = [&](auto bf, auto sts) {
         k_router<l, v, decltype(bf)::value, decltype(sts)::value><<<grid, kThreads, shm, s>>>(
             g, logits, tok->mask, tok->seq_start, by_rollout, expert_ids, gates, lse, w);
@@ -870,14 +1036,14 @@ rft_status rft_router_bwd(const rft_tokens* tok, const void* logits, int dtype, 
     return fail(RFT_E_SHAPE, "%s: d_logits is logits with another row stride", fn);
   if (tok->T == 0) return RFT_OK;
   const bool by_rollout = params->scope == RFT_BALANCE_ROLLOUT;
-  const Geom g = geometry(*tok, *params, logits, dtype, ld);
-  const bool dvec = geometry(*tok, *params, d_logits, dtype, ldd).vec;
-  const unsigned grid = (unsigned)((g.nW + kWaves - 1) / kWaves);
+  const Geom g = geometry(*tok, *params, logits, dtype, ld, kBwdWaves);
+  const bool dvec = geometry(*tok, *params, d_logits, dtype, ldd, kBwdWaves).vec;
+  const unsigned grid = (unsigned)((g.nW + kBwdWavesPer - 1) / kBwdWavesPer);
   hipStream_t s = (hipStream_t)stream;
   by_experts(g.E, [&](auto L, auto V) {
     constexpr int l = decltype(L)::value, v = decltype(V)::value;
     auto go = [&](auto bf) {
-      k_router_bwd<l, v, decltype(bf)::value><<<grid, kThreads, 0, s>>>(
+      k_router_bwd<l, v, decltype(bf)::value><<<grid, kBwdThreads, 0, s>>>(
           g, logits, tok->mask, tok->seq_start, by_rollout, expert_ids, lse, d_gates, dprob, stats,
           params->balance_coef, params->z_coef, d_logits, ldd, dvec);
     };
