@@ -20,11 +20,12 @@
 // lo hi (what is left out is 2^-22 of a product): errors as of fp32 products at three
 // times the instructions, where the card's fp32 instructions would take sixteen.
 //
-// Layout.  Operands are stored in blocks of 128 rows x 64 columns (16 KiB, row-major
-// inside), the blocks of a 128-row panel side by side, padded with zeros to multiples of
-// 128: each k-step of a tile is one contiguous block per operand, copied straight to
-// LDS.  X is kept both ways round (X^T is the operand of APPLY); GRAM and POLY are
-// symmetric and compute the tiles on and above the diagonal, storing each both ways.
+// Layout.  Operands are stored in blocks of 128 rows x 32 columns (8 KiB, row-major inside),
+// the blocks of a 128-row panel side by side, padded with zeros to multiples of 128 rows and
+// columns: a k-step of a tile is contiguous blocks, copied straight to LDS.  In APPLY the rows
+// of X are the summed index; its tiles of 32 rows are read from LDS transposed
+// (ds_read_b64_tr_b16), so no transposed copy of X exists.  GRAM and POLY are symmetric and
+// compute the tiles on and above the diagonal, storing each both ways round.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -36,13 +37,14 @@ namespace ns {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr int kPad = 128;  // rows and columns are padded to it
-constexpr int BK = 64;
-constexpr int64_t kBlk = 128 * BK;  // elements of a block
+constexpr int BC = 32;     // columns of a block
+constexpr int64_t kBlk = 128 * BC;      // elements of a block
+constexpr int kBlkBytes = 128 * BC * 2;
 // entries of X, O and P stay below 16 in magnitude (a condition on the coefficients)
 constexpr float kScale = 4096.f, kInv = 1.f / 4096.f;
 
@@ -50,7 +52,7 @@ enum { GRAM = 0, POLY = 1, APPLY = 2, LAST = 3 };
 
 // Element (r, c) of a blocked matrix with kp columns.
 __host__ __device__ __forceinline__ int64_t blk_at(int64_t r, int64_t c, int64_t kp) {
-  return ((r >> 7) * (kp >> 6) + (c >> 6)) * kBlk + (r & 127) * BK + (c & 63);
+  return ((r >> 7) * (kp >> 5) + (c >> 5)) * kBlk + (r & 127) * BC + (c & 31);
 }
 
 // A blocked matrix as hi + lo planes (lo may be nullptr), matrices `step` apart.
@@ -61,6 +63,7 @@ struct Mat {
 
 struct Result {  // of LAST
   int flip;      // X is the transpose of the caller's matrix
+  int vec;       // four elements of a row at a time (alignment, strides)
   int64_t rows, cols, row_stride, batch_stride;
   void* out;     // rft_orthogonalize: out = scale X
   int out_bf16;
@@ -72,11 +75,12 @@ struct Result {  // of LAST
 };
 
 struct Args {
-  Mat A, B;      // operands: rows of A against rows of B
+  Mat A, B;      // operands: rows of A against rows of B (APPLY, LAST: columns of B)
+  int pa, pb;    // 128-row panels of A, of B (APPLY, LAST: 128-column panels)
   int K;         // padded
   int tm, tn;    // tiles of C
   int sym;       // only tiles j >= i
-  Mat X, Xt, O, P;
+  Mat X, Y, O, P;  // APPLY: Y = p X + P X
   float *d, *p;  // [batch, mp]
   int mp, np;
   float a, b, c;
@@ -100,39 +104,46 @@ __device__ __forceinline__ f16x4 hi_of(floatx4 x) { return __builtin_convertvect
 __device__ __forceinline__ f16x4 lo_of(floatx4 x, f16x4 h) {
   return __builtin_convertvector(x - __builtin_convertvector(h, floatx4), f16x4);
 }
-__device__ __forceinline__ floatx4 join(f16x4 h) { return __builtin_convertvector(h, floatx4); }
-
-// 128 x 128 tile, four waves of 64 x 64 (4 x 4 tiles of 16 x 16).
-constexpr int NT = 256;
-constexpr int OPB = 128 * BK * 2;  // bytes of an operand block in LDS
-constexpr int PITCH = 272;         // bytes of a staged row of 128 fp16
-
-// Copies a staged 128 x 128 tile (rows PITCH bytes apart) to two blocks (32 KiB).
-__device__ __forceinline__ void copy_out(const char* st, _Float16* dst, int tid) {
-#pragma unroll
-  for (int it = 0; it < 8; ++it) {
-    const int c = it * NT + tid, row = c >> 4, ch = c & 15;
-    const u32x4 v = *(const u32x4*)(st + row * PITCH + ch * 16);
-    *(u32x4*)(dst + (ch >> 3) * kBlk + row * BK + (ch & 7) * 8) = v;
-  }
+__device__ __forceinline__ floatx4 join(const _Float16* p) {
+  return __builtin_convertvector(*(const f16x4*)p, floatx4);
 }
 
-template <int PROD, int EPI, bool FLIP>
+// Four rows (4 g .. of lane group g) of column lane % 16 from a 16-lane group's rows at p:
+// lane s of a group reads columns 4 (s % 4) .. of row s / 4 of its own.
+__device__ __forceinline__ s16x4 read_tr(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+}
+
+// s_waitcnt vmcnt(N), the other counters left alone.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | 0x0F70 | ((N >> 4) << 14));
+}
+
+// Tiles of 128 TP x 128 TP, eight waves (two per SIMD: the loads and LDS reads of one go
+// out while the other multiplies) of 64 x 32 (TP = 1) or 64 x 128 (TP = 2), KB blocks of 32
+// columns per stage, NS stages in LDS of which NS - 1 are on their way.
+constexpr int NT = 512;
+template <int PROD, int EPI, bool FLIP, int TP, int NS>
 __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   constexpr int NOP = PROD == 3 ? 2 : 1;  // planes per operand
+  constexpr int KB = PROD == 3 ? 1 : 2;
+  constexpr bool TR = EPI == APPLY || EPI == LAST;
+  constexpr int OPB = KB * TP * kBlkBytes;  // bytes of an operand plane in a stage
   constexpr int STAGE = 2 * NOP * OPB;
-  // operands of the matrix instruction in the order that gives a lane four consecutive
-  // columns of C (rows where the result is stored transposed)
-  constexpr bool ROWS4 = EPI == LAST && FLIP;
-  __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
+  constexpr int WC = TP == 1 ? 4 : 2;       // waves along the columns
+  constexpr int WN = 8 * TP / WC;           // 16-column tiles of a wave
+  constexpr int SETS = TP == 1 ? 2 : 1;     // of fragments in registers
+  constexpr int SB = TP == 1 ? 2 : 1;       // rows of tiles whose epilogue operands are held
+  __shared__ __attribute__((aligned(16))) char lds[NS * STAGE];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wid >> 1, wn = wid & 1;
+  const int wm = wid / WC, wn = wid % WC;  // 2 TP x WC waves
   const int r16 = lane & 15, q4 = lane >> 4;
   const int bt = blockIdx.y;
   int ti, tj;
   {
-    int t = blockIdx.x;
+    const int t = blockIdx.x;
     if (g.sym) {
       // column by column of the upper triangle: tj (tj + 1) / 2 <= t
       tj = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
@@ -144,148 +155,317 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
       tj = t / g.tm;
     }
   }
-  const int64_t panel = (int64_t)128 * g.K;
-  const int64_t oA = bt * g.A.step + ti * panel, oB = bt * g.B.step + tj * panel;
-  const __amdgpu_buffer_rsrc_t rA = rsrc(g.A.hi + oA, (int)(panel * 2));
-  const __amdgpu_buffer_rsrc_t rB = rsrc(g.B.hi + oB, (int)(panel * 2));
-  const __amdgpu_buffer_rsrc_t rAl = rsrc((NOP == 2 ? g.A.lo : g.A.hi) + oA, (int)(panel * 2));
-  const __amdgpu_buffer_rsrc_t rBl = rsrc((NOP == 2 ? g.B.lo : g.B.hi) + oB, (int)(panel * 2));
-  // LDS rows of 128 bytes, 16-byte chunk c of row r at chunk c ^ ((r >> 1) & 7): the
-  // fragment reads of 16 lanes then touch every bank once.  A wave copies 32 rows of
-  // each operand, eight per instruction; lane l fills chunk l % 8 of row l / 8.
-  uint32_t vq[2];
-#pragma unroll
-  for (int q = 0; q < 2; ++q)
-    vq[q] = (uint32_t)((lane >> 3) * 128 + (((lane & 7) ^ (lane >> 4) ^ (q * 4)) << 4));
-  auto load1 = [&](__amdgpu_buffer_rsrc_t r, char* dst, int kt) {
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const int at = (wid * 4 + p) * 1024;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(dst + at), 16,
-                                               vq[p & 1] + (uint32_t)at, kt * (int)(kBlk * 2), 0, 0);
+  // Descriptors: the tile's panels that exist (everything past them reads as 0); in TR that of
+  // B covers the 128 rows of X that a k-step lies in, and moves on with k.
+  const int panel = g.K * 256;                       // bytes of a panel of A (and of B)
+  const int64_t oA = bt * g.A.step + (int64_t)ti * TP * (panel / 2);
+  const int nA = min(TP, g.pa - ti * TP) * panel;
+  const __amdgpu_buffer_rsrc_t rA = rsrc(g.A.hi + oA, nA);
+  const __amdgpu_buffer_rsrc_t rAl = rsrc((NOP == 2 ? g.A.lo : g.A.hi) + oA, nA);
+  const int rowsB = TR ? g.np * 256 : panel;         // bytes of 128 rows of B
+  const int64_t oB = bt * g.B.step + (TR ? 0 : (int64_t)tj * TP * (panel / 2));
+  const int nB = TR ? rowsB : min(TP, g.pb - tj * TP) * panel;
+  const __amdgpu_buffer_rsrc_t rB = rsrc(g.B.hi + oB, nB);
+  const __amdgpu_buffer_rsrc_t rBl = rsrc((NOP == 2 ? g.B.lo : g.B.hi) + oB, nB);
+  // LDS rows of 64 bytes.  Read along the rows (a 16-byte chunk of 16 rows by each of four
+  // lane groups): chunk c of row r lies at c ^ key((r >> 2) & 3), key 0 2 3 1, with which the
+  // lanes that ds_read_b128 serves together (0-3, 12-15, 20-23, 24-27, then 4-11, 16-19,
+  // 28-31, and the same 32 lanes on) touch every bank once; c ^ ((r >> 2) & 3) gave two-way
+  // conflicts.  Read transposed (two groups of four rows, 32 bytes each, eight rows apart):
+  // chunk c at c ^ 2 ((r >> 3) & 1).
+  // A load fills 16 rows (1 KiB); lane l chunk l % 4 of row l / 4.
+  auto key = [](int x) { return (0x78 >> (2 * (x & 3))) & 3; };
+  const uint32_t vr = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ key(lane >> 4)) << 4));
+  const uint32_t vt = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ (((lane >> 5) & 1) << 1)) << 4));
+  constexpr int NI = KB * TP;  // instructions per wave, operand plane and stage
+  // What may pass a descriptor's end goes into the vector part of the offset, which is what
+  // the hardware compares; a stage past the last reads zeros (off = 2^31), so that the loop
+  // has no branches.
+  auto load_row = [&](__amdgpu_buffer_rsrc_t r, char* dst, int kt, uint32_t off, int p) {
+    const int q = wid * NI + p, kb = q / (8 * TP), pn = (q >> 3) % TP, part = q & 7;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        r, (lds_ptr)(dst + q * 1024), 16,
+        vr + ((uint32_t)(pn * panel + kb * kBlkBytes + part * 1024) | off), kt * KB * kBlkBytes, 0, 0);
+  };
+  // 32 rows (from 32 kt KB on) x 128 TP columns: 4 TP blocks' 2 KiB pieces
+  auto load_col = [&](__amdgpu_buffer_rsrc_t r, char* dst, int kt, uint32_t off, int p) {
+    const int q = wid * NI + p, kb = q / (8 * TP), cb = (q >> 1) % (4 * TP), half = q & 1;
+    const int k0 = (kt * KB & 3) * 32;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        r, (lds_ptr)(dst + q * 1024), 16,
+        vt + ((uint32_t)((tj * 4 * TP + cb) * kBlkBytes + kb * 2048 + half * 1024) | off), k0 * 64, 0, 0);
+  };
+  const int nk = g.K / (BC * KB);  // K is a multiple of 128: nk is even where KB = 1
+  constexpr int L = 2 * NOP * NI;  // load instructions per wave and stage
+  // The x-th load of stage t: operand planes A, B, and of lo planes A, B, NI each.
+  auto load_one = [&](char* dst, int t, int x) {
+    const int kt = t < nk ? t : 0, plane = x / NI, p = x % NI;
+    const uint32_t off = t < nk ? 0u : 0x80000000u;
+    const bool lo = plane >= 2;
+    char* const d = dst + plane * OPB;
+    if (plane % 2 == 0) {
+      load_row(lo ? rAl : rA, d, kt, off, p);
+    } else if (TR) {
+      const int64_t o = oB + (int64_t)(kt * KB >> 2) * (rowsB / 2);
+      load_col(rsrc((lo ? g.B.lo : g.B.hi) + o, rowsB), d, kt, off, p);
+    } else {
+      load_row(lo ? rBl : rB, d, kt, off, p);
     }
   };
-  auto load = [&](char* dst, int kt) {  // operand blocks A, B, and of lo planes A, B
-    load1(rA, dst, kt);
-    load1(rB, dst + OPB, kt);
-    if (NOP == 2) {
-      load1(rAl, dst + 2 * OPB, kt);
-      load1(rBl, dst + 3 * OPB, kt);
-    }
+  auto load = [&](char* dst, int t) {
+#pragma unroll
+    for (int x = 0; x < L; ++x) load_one(dst, t, x);
   };
-  floatx4 acc[4][4];
+  floatx4 acc[4][WN];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
-  const int nk = g.K / BK;
-  load(lds, 0);
-  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
-  __syncthreads();
-  for (int kt = 0; kt < nk; ++kt) {
-    if (kt + 1 < nk) load(lds + ((kt + 1) & 1) * STAGE, kt + 1);
-    const char* st = lds + (kt & 1) * STAGE;
+    for (int j = 0; j < WN; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const int cho = ((ks * 4 + q4) ^ ((r16 >> 1) & 7)) << 4;
-      f16x8 a[NOP][4], b[NOP][4];
-#pragma unroll
-      for (int o = 0; o < NOP; ++o)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          a[o][i] = *(const f16x8*)(st + (2 * o) * OPB + (wm * 64 + i * 16 + r16) * 128 + cho);
-          b[o][i] = *(const f16x8*)(st + (2 * o + 1) * OPB + (wn * 64 + i * 16 + r16) * 128 + cho);
-        }
-#pragma unroll
-      for (int pr = 0; pr < PROD; ++pr) {  // hi hi, then hi lo and lo hi
-        const int oa = pr == 2 ? 1 : 0, ob = pr == 1 ? 1 : 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            acc[i][j] = ROWS4 ? __builtin_amdgcn_mfma_f32_16x16x32_f16(a[oa][i], b[ob][j], acc[i][j], 0, 0, 0)
-                              : __builtin_amdgcn_mfma_f32_16x16x32_f16(b[ob][j], a[oa][i], acc[i][j], 0, 0, 0);
-      }
+  for (int p = 0; p < NS; ++p) load(lds + p * STAGE, p);
+  const int cr = (q4 ^ key(r16 >> 2)) << 4;  // chunk of a row-wise fragment
+  // a transposed fragment: rows 8 q4 + 4 h + (r16 >> 2), columns 4 (r16 & 3) .. of 16
+  const int rt = 8 * q4 + (r16 >> 2);
+  const int ct0 = ((r16 & 3) >> 1), ct1 = (r16 & 1) * 8;
+  // The x-th of a set's RD fragment reads (of 32 columns), the q-th of its PD products.
+  constexpr int BR = TR ? 2 * WN : WN, RD = NOP * (4 + BR), PD = PROD * 4 * WN;
+  f16x8 fa[SETS][NOP][4], fb[SETS][NOP][WN];
+  s16x4 fh[SETS][NOP][WN][2];  // TR: halves of fb
+  auto read_one = [&](int set, const char* st, int kb, int x) {
+    const int o = x / (4 + BR), y = x % (4 + BR);
+    const char* sa = st + 2 * o * OPB + kb * (TP * kBlkBytes) + (wm * 64 + r16) * 64 + cr;
+    const char* sb = st + (2 * o + 1) * OPB + kb * (TP * kBlkBytes);
+    if (y < 4) {
+      fa[set][o][y] = *(const f16x8*)(sa + y * 1024);
+    } else if (TR) {
+      // 16 columns 16 (wn WN + j) .. : half j % 2 of a block's 2 KiB
+      const int j = (y - 4) / 2, u = (y - 4) % 2;
+      const int row = rt + 4 * u, c = ((j & 1) * 2 + ct0) ^ ((q4 & 1) << 1);
+      fh[set][o][j][u] = read_tr(sb + (wn * (WN / 2) + (j >> 1)) * 2048 + row * 64 + c * 16 + ct1);
+    } else {
+      fb[set][o][y - 4] = *(const f16x8*)(sb + (wn * 16 * WN + r16) * 64 + (y - 4) * 1024 + cr);
     }
-    // this wave's loads of the next stage have landed and its reads of this one are done
-    // before the barrier that lets the next loads overwrite it
-    __builtin_amdgcn_s_waitcnt(0x0F70);
+  };
+  auto multiply_one = [&](int set, int q) {  // hi hi, then hi lo and lo hi
+    const int pr = q / (4 * WN), i = q / WN % 4, j = q % WN, oa = pr == 2 ? 1 : 0, ob = pr == 1 ? 1 : 0;
+    const f16x8 b = TR ? __builtin_bit_cast(f16x8, __builtin_shufflevector(
+                             fh[set][ob][j][0], fh[set][ob][j][1], 0, 1, 2, 3, 4, 5, 6, 7))
+                       : fb[set][ob][j];
+    // operands in the order that gives a lane four consecutive columns of C
+    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, fa[set][oa][i], acc[i][j], 0, 0, 0);
+  };
+  // Stage t lies in buffer t % NS.  `turn` makes stage kt + 1 readable: this wave's loads of
+  // it have landed (those after it may be under way) and its reads of stage kt are done; then
+  // every wave's, and stage kt's buffer can take stage kt + NS.
+  wait_vm<(NS - 1) * L>();
+  barrier_lds();
+  int cur = 0;  // kt % NS
+  auto turn = [&]() {
+    wait_vm<(NS - 2) * L>();
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     barrier_lds();
+  };
+  if constexpr (SETS == 2) {
+    // Few products per fragment: the fragments of the next 32 columns are read, and the next
+    // stage's loads issued, between the products of this one.
+    constexpr int UN = KB == 1 ? 2 : 1;  // stages per turn of the loop: the sets alternate
+#pragma unroll
+    for (int x = 0; x < RD; ++x) read_one(0, lds, 0, x);
+    for (int kt = 0; kt < nk; kt += UN) {
+#pragma unroll
+      for (int u = 0; u < UN * KB; ++u) {
+        const int set = u & 1, k1 = kt + u / KB;
+        const bool last = (u + 1) % KB == 0;  // of its stage
+        char* const old = lds + cur * STAGE;
+        if (last) {
+          turn();
+          cur = cur == NS - 1 ? 0 : cur + 1;
+        }
+        const char* const st = lds + cur * STAGE;
+        const int extra = RD + (last ? L : 0);
+#pragma unroll
+        for (int q = 0; q < PD; ++q) {
+          multiply_one(set, q);
+          // past the last stage the reads are not used
+#pragma unroll
+          for (int x = q * extra / PD; x < (q + 1) * extra / PD; ++x) {
+            if (x < RD)
+              read_one(set ^ 1, st, (u + 1) % KB, x);
+            else
+              load_one(old, k1 + NS, x - RD);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+  } else {
+    // two waves per SIMD: one reads while the other multiplies
+    for (int kt = 0; kt < nk; ++kt) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+        for (int x = 0; x < RD; ++x) read_one(0, lds + cur * STAGE, kb, x);
+#pragma unroll
+        for (int q = 0; q < PD; ++q) multiply_one(0, q);
+      }
+      turn();
+      load(lds + cur * STAGE, kt + NS);
+      cur = cur == NS - 1 ? 0 : cur + 1;
+    }
   }
+  wait_vm<0>();
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  barrier_lds();  // no load is under way, the stages are free
 
   // ------------------------------------------------------------------ epilogue
-  const int i0 = ti * 128 + wm * 64, j0 = tj * 128 + wn * 64;
+  // element q of tile (i, j): row i0 + 16 i + r16, column j0 + 16 j + 4 q4 + q
+  const int i0 = (ti * TP + (wm >> 1)) * 128 + (wm & 1) * 64, j0 = tj * TP * 128 + wn * 16 * WN;
+  char* const mine = lds + wid * 2048;  // of this wave: a 16 x 16 tile at a time
+  if (i0 >= g.mp) return;
+  // What a row of tiles needs from memory is loaded whole, that of the next row before this
+  // one's results are stored (one load at a time, in order with the stores, took
+  // longer than the products of small matrices).
   if constexpr (EPI == LAST) {
     const Result& r = g.r;
     if (r.clip && !r.clip->finite) return;
-    const float* p = g.p + (int64_t)bt * g.mp;
-    const int64_t xb = bt * g.X.step;
     const int64_t M = r.flip ? r.cols : r.rows, N = r.flip ? r.rows : r.cols;
+    const int64_t end = FLIP ? M : N;
+    const float f = kInv * r.scale;
+    f16x4 sh[SB][WN], sl[SB][WN];
+    float pi[SB];
+    floatx4 w[WN];
+    auto state = [&](int i, int to) {
+      const int row = i0 + i * 16 + r16;
+      pi[to] = g.p[(int64_t)bt * g.mp + row];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int j = 0; j < WN; ++j) {
+        if (j0 + j * 16 >= g.np) continue;
+        const int64_t o = bt * g.X.step + blk_at(row, j0 + j * 16 + q4 * 4, g.np);
+        sh[to][j] = *(const f16x4*)(g.X.hi + o);
+        sl[to][j] = *(const f16x4*)(g.X.lo + o);
+      }
+    };
+    // four consecutive elements (u, v) .. of a row of the caller's matrix
+    auto place = [&](int i, int j, int64_t& v) {
+      const int64_t u = FLIP ? j0 + j * 16 + r16 : i0 + i * 16 + r16;
+      v = FLIP ? i0 + i * 16 + q4 * 4 : j0 + j * 16 + q4 * 4;
+      if (u >= (FLIP ? N : M)) v = end;
+      return bt * r.batch_stride + u * r.row_stride + v;
+    };
+    auto old = [&](int i, int j) {  // the weights' tile, where four can be taken at a time
+      int64_t v;
+      const int64_t at = place(i, j, v);
+      if (!r.weight || !r.vec || j0 + j * 16 >= g.np || v >= end) return;
+      if (r.master) {
+        w[j] = *(const floatx4*)(r.master + at);
+      } else if (r.weight_bf16) {
+        const u16x4 h = *(const u16x4*)((const uint16_t*)r.weight + at);
+        w[j] = (floatx4){bf16_to_f32(h[0]), bf16_to_f32(h[1]), bf16_to_f32(h[2]), bf16_to_f32(h[3])};
+      } else {
+        w[j] = *(const floatx4*)((const float*)r.weight + at);
+      }
+    };
+    if (SB == 2) state(0, 0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        // four consecutive elements of a row of the caller's matrix, from (u, v)
-        float x[4];
-        int64_t u, v, vend;
-        if (ROWS4) {
-          const int row = i0 + i * 16 + q4 * 4, col = j0 + j * 16 + r16;
+    for (int i = 0; i < 4; ++i) {
+      if (SB == 1) state(i, 0);
+      if (SB == 2) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int64_t o = xb + blk_at(row + q, col, g.np);
-            x[q] = p[row + q] * ((float)g.X.hi[o] + (float)g.X.lo[o]) + acc[i][j][q] * kInv;
-          }
-          u = col;
-          v = row;
-          vend = u < N ? M : 0;
-        } else {
-          const int row = i0 + i * 16 + r16, col = j0 + j * 16 + q4 * 4;
-          const int64_t o = xb + blk_at(row, col, g.np);
-          const floatx4 s = join(*(const f16x4*)(g.X.hi + o)) + join(*(const f16x4*)(g.X.lo + o));
+        for (int j = 0; j < WN; ++j) old(i, j);
+      }
+      if (SB == 2 && i + 1 < 4) state(i + 1, (i + 1) & 1);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) x[q] = p[row] * s[q] + acc[i][j][q] * kInv;
-          u = row;
-          v = col;
-          vend = u < M ? N : 0;
+      for (int j = 0; j < WN; ++j) {
+        if (j0 + j * 16 >= g.np) continue;
+        const floatx4 x = __builtin_convertvector(sh[i % SB][j], floatx4) +
+                          __builtin_convertvector(sl[i % SB][j], floatx4);
+        floatx4 y = (pi[i % SB] * x + acc[i][j] * kInv) * f;
+        if (FLIP) {  // the tile transposed through LDS, rows 20 floats apart
+          float* const t = (float*)mine;
+          __builtin_amdgcn_wave_barrier();
+          *(floatx4*)(t + r16 * 20 + q4 * 4) = y;
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int q = 0; q < 4; ++q) y[q] = t[(q4 * 4 + q) * 20 + r16];
         }
-        const int64_t at = bt * r.batch_stride + u * r.row_stride + v;
+        int64_t v;
+        const int64_t at = place(i, j, v);
+        if (v >= end) continue;
+        if (SB == 1) old(i, j);
+        void* const dst = r.weight ? r.weight : r.out;
+        const bool half = r.weight ? r.weight_bf16 : r.out_bf16;
+        if (r.vec) {
+          if (r.weight) {
+            y = w[j] * r.decay - y;
+            if (r.master) *(floatx4*)(r.master + at) = y;
+          }
+          if (half)
+            *(u16x4*)((uint16_t*)dst + at) = (u16x4){f32_to_bf16(y[0]), f32_to_bf16(y[1]),
+                                                     f32_to_bf16(y[2]), f32_to_bf16(y[3])};
+          else
+            *(floatx4*)((float*)dst + at) = y;
+          continue;
+        }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          if (v + q >= vend) continue;
-          const float y = x[q] * (kInv * r.scale);
+          if (v + q >= end) continue;
+          float z = y[q];
           if (r.weight) {
             const float w0 = r.master ? r.master[at + q]
                              : r.weight_bf16 ? bf16_to_f32(((const uint16_t*)r.weight)[at + q])
                                              : ((const float*)r.weight)[at + q];
-            const float w = w0 * r.decay - y;
-            if (r.master) r.master[at + q] = w;
-            if (r.weight_bf16)
-              ((uint16_t*)r.weight)[at + q] = f32_to_bf16(w);
-            else
-              ((float*)r.weight)[at + q] = w;
-          } else if (r.out_bf16) {
-            ((uint16_t*)r.out)[at + q] = f32_to_bf16(y);
-          } else {
-            ((float*)r.out)[at + q] = y;
+            z = w0 * r.decay - z;
+            if (r.master) r.master[at + q] = z;
           }
+          if (half)
+            ((uint16_t*)dst)[at + q] = f32_to_bf16(z);
+          else
+            ((float*)dst)[at + q] = z;
         }
       }
+    }
   } else {
-    // kScale times the new values, four columns of a row each
-    const Mat& dst = EPI == GRAM ? g.O : EPI == POLY ? g.P : g.X;
+    const Mat& dst = EPI == GRAM ? g.O : EPI == POLY ? g.P : g.Y;
+    const Mat& src = EPI == POLY ? g.O : g.X;
+    constexpr bool HI = EPI != GRAM, LO = EPI == APPLY || (EPI == POLY && NOP == 2);
     const int kp = EPI == APPLY ? g.np : g.mp;
     const int64_t vb = (int64_t)bt * g.mp;
+    const bool mirror = EPI != APPLY && ti != tj;
+    f16x4 sh[SB][WN], sl[SB][WN];
+    float di[SB] = {};
+    auto state = [&](int i, int to) {
+      const int row = i0 + i * 16 + r16;
+      if (EPI == POLY) di[to] = g.d[vb + row];
+      if (EPI == APPLY) di[to] = g.p[vb + row];
+#pragma unroll
+      for (int j = 0; j < WN; ++j) {
+        if (!HI || j0 + j * 16 >= kp) continue;
+        const int64_t o = bt * src.step + blk_at(row, j0 + j * 16 + q4 * 4, kp);
+        sh[to][j] = *(const f16x4*)(src.hi + o);
+        if (LO) sl[to][j] = *(const f16x4*)(src.lo + o);
+      }
+    };
+    floatx4 dj[WN];
+    if (EPI == POLY && SB == 2) {
+#pragma unroll
+      for (int j = 0; j < WN; ++j)
+        if (j0 + j * 16 < kp) dj[j] = *(const floatx4*)(g.d + vb + j0 + j * 16 + q4 * 4);
+    }
+    if (SB == 2) state(0, 0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = i0 + i * 16 + r16;
-      float di = 0.f;
-      if (EPI == POLY) di = g.d[vb + row];
-      if (EPI == APPLY) di = g.p[vb + row];
+      if (SB == 1) state(i, 0);
+      if (SB == 2 && i + 1 < 4) state(i + 1, (i + 1) & 1);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < WN; ++j) {
         const int col = j0 + j * 16 + q4 * 4;
-        floatx4 x = acc[i][j] * kInv;
+        if (j0 + j * 16 >= kp) continue;
+        const int64_t o = blk_at(row, col, kp);
+        floatx4 x = acc[i][j] * kInv;  // kScale times the new values
+        floatx4 s = {0.f, 0.f, 0.f, 0.f};
+        if (HI) s = __builtin_convertvector(sh[i % SB][j], floatx4);
+        if (LO) s += __builtin_convertvector(sl[i % SB][j], floatx4);
         if constexpr (EPI == GRAM) {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
@@ -294,64 +474,44 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
               x[q] = 0.f;
             }
         } else if constexpr (EPI == POLY) {
-          const int64_t o = bt * g.O.step + blk_at(row, col, g.mp);
-          floatx4 s = join(*(const f16x4*)(g.O.hi + o));
-          if (NOP == 2) s += join(*(const f16x4*)(g.O.lo + o));
-          const floatx4 dj = *(const floatx4*)(g.d + vb + col);
+          const float dr = di[i % SB];
+          if (SB == 1) dj[j] = *(const floatx4*)(g.d + vb + col);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             if (row == col + q) {
-              g.p[vb + row] = g.a + g.b * di + g.c * (x[q] * kInv + di * di);
+              g.p[vb + row] = g.a + g.b * dr + g.c * (x[q] * kInv + dr * dr);
               x[q] = 0.f;
             } else {
-              x[q] = g.b * s[q] + g.c * (x[q] + (di + dj[q]) * s[q]);
+              x[q] = g.b * s[q] + g.c * (x[q] + (dr + dj[j][q]) * s[q]);
             }
           }
         } else {
-          const int64_t o = bt * g.X.step + blk_at(row, col, g.np);
-          const floatx4 s = join(*(const f16x4*)(g.X.hi + o)) + join(*(const f16x4*)(g.X.lo + o));
-          x += di * s;
+          x += di[i % SB] * s;
         }
-        acc[i][j] = x;
+        const f16x4 h = hi_of(x);
+        *(f16x4*)(dst.hi + bt * dst.step + o) = h;
+        // lo planes: of X always, of the others where products use them
+        f16x4 l;
+        if (EPI == APPLY || NOP == 2) {
+          l = lo_of(x, h);
+          *(f16x4*)(dst.lo + bt * dst.step + o) = l;
+        }
+        if (mirror) {
+          // the 16 x 16 tile through LDS (rows of 32 bytes, read transposed): lane holds
+          // rows 4 q4 .. of column r16, four consecutive elements of the mirrored row
+          const int64_t om = bt * dst.step + blk_at(j0 + j * 16 + r16, i0 + i * 16 + q4 * 4, kp);
+          __builtin_amdgcn_wave_barrier();
+          *(f16x4*)(mine + r16 * 32 + q4 * 8) = h;
+          if (NOP == 2) *(f16x4*)(mine + 512 + r16 * 32 + q4 * 8) = l;
+          __builtin_amdgcn_wave_barrier();
+          const s16x4 th = read_tr(mine + lane * 8);
+          *(s16x4*)(dst.hi + om) = th;
+          if (NOP == 2) {
+            const s16x4 tl = read_tr(mine + 512 + lane * 8);
+            *(s16x4*)(dst.lo + om) = tl;
+          }
+        }
       }
-    }
-    // stored tile by tile through LDS, each way round: 16 bytes per lane
-    const int lrow = wm * 64 + r16, lcol = wn * 64 + q4 * 4;
-    const bool mirror = EPI == APPLY || ti != tj;
-    const Mat& tr = EPI == APPLY ? g.Xt : dst;
-    const int kt_ = g.mp;
-#pragma unroll
-    for (int plane = 0; plane < 2; ++plane) {
-      // lo planes: of X always, of the others where products use them
-      if (plane == 1 && EPI != APPLY && NOP == 1) break;
-      f16x4 h[4][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          h[i][j] = hi_of(acc[i][j]);
-          if (plane == 1) h[i][j] = lo_of(acc[i][j], h[i][j]);
-        }
-      char* const st = lds;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *(f16x4*)(st + (lrow + i * 16) * PITCH + (lcol + j * 16) * 2) = h[i][j];
-      __syncthreads();
-      copy_out(st, (plane ? dst.lo : dst.hi) + bt * dst.step + blk_at(ti * 128, tj * 128, kp), tid);
-      if (!mirror || (plane == 1 && NOP == 1)) continue;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *(_Float16*)(st + (lcol + j * 16 + q) * PITCH + (lrow + i * 16) * 2) = h[i][j][q];
-      __syncthreads();
-      copy_out(st, (plane ? tr.lo : tr.hi) + bt * tr.step + blk_at(tj * 128, ti * 128, kt_), tid);
     }
   }
 }
@@ -359,6 +519,7 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
 // ---------------------------------------------------------------- the input --
 struct Input {
   int64_t rows, cols, row_stride, batch_stride;
+  int vec;     // four elements of a row at a time (alignment, strides)
   const void* g;
   int bf16;
   float* buf;  // momentum, or nullptr
@@ -368,19 +529,91 @@ struct Input {
   double eps;
 };
 
-__device__ __forceinline__ float grad_at(const Input& in, int64_t o, float scale) {
-  return scale * (in.bf16 ? bf16_to_f32(((const uint16_t*)in.g)[o]) : ((const float*)in.g)[o]);
+template <int V>
+struct Vals {
+  float v[V];
+};
+template <int V>
+__device__ __forceinline__ Vals<V> grad_at(const Input& in, int64_t o, float scale) {
+  Vals<V> r;
+  if constexpr (V == 4) {
+    if (in.bf16) {
+      const u16x4 h = *(const u16x4*)((const uint16_t*)in.g + o);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) r.v[q] = scale * bf16_to_f32(h[q]);
+    } else {
+      const floatx4 h = *(const floatx4*)((const float*)in.g + o);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) r.v[q] = scale * h[q];
+    }
+  } else {
+    r.v[0] = scale * (in.bf16 ? bf16_to_f32(((const uint16_t*)in.g)[o]) : ((const float*)in.g)[o]);
+  }
+  return r;
 }
-// The update's element before orthogonalisation, from the momentum already updated.
-__device__ __forceinline__ float update_at(const Input& in, int64_t o, float scale) {
-  if (!in.buf) return grad_at(in, o, scale);
-  const float b = in.buf[o];
-  return in.nesterov ? fmaf(in.mu, b, in.nu * grad_at(in, o, scale)) : b;
+// The update before orthogonalisation, from the momentum b already updated.
+template <int V>
+__device__ __forceinline__ Vals<V> update_from(const Input& in, const Vals<V>& g, const Vals<V>& b) {
+  Vals<V> u = b;
+  if (in.nesterov)
+#pragma unroll
+    for (int q = 0; q < V; ++q) u.v[q] = fmaf(in.mu, b.v[q], in.nu * g.v[q]);
+  return u;
+}
+template <int V>
+__device__ __forceinline__ Vals<V> buf_at(const Input& in, int64_t o) {
+  Vals<V> r;
+  if constexpr (V == 4) {
+    const floatx4 b = *(const floatx4*)(in.buf + o);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) r.v[q] = b[q];
+  } else {
+    r.v[0] = in.buf[o];
+  }
+  return r;
+}
+template <int V>
+__device__ __forceinline__ Vals<V> update_at(const Input& in, int64_t o, float scale) {
+  if (!in.buf) return grad_at<V>(in, o, scale);
+  const Vals<V> b = buf_at<V>(in, o);
+  if (!in.nesterov) return b;
+  return update_from<V>(in, grad_at<V>(in, o, scale), b);
 }
 
 // Block (chunk, matrix): momentum of `per` elements and the sum of squares of the update
 // in fp64.
 constexpr int kInT = 256;
+template <int V>
+__device__ __forceinline__ double norm_chunk(const Input& in, int64_t e0, int64_t e1, int64_t base,
+                                             float scale) {
+  double s = 0;
+  const int64_t step = kInT * V, dr = step / in.cols, dc = step - dr * in.cols;
+  int64_t r = (e0 + threadIdx.x * V) / in.cols, c = (e0 + threadIdx.x * V) - r * in.cols;
+#pragma unroll 4
+  for (int64_t e = e0 + threadIdx.x * V; e < e1; e += step) {
+    const int64_t o = base + r * in.row_stride + c;
+    Vals<V> u = grad_at<V>(in, o, scale);
+    if (in.buf) {
+      Vals<V> b = buf_at<V>(in, o);
+#pragma unroll
+      for (int q = 0; q < V; ++q) b.v[q] = fmaf(in.mu, b.v[q], in.nu * u.v[q]);
+      if constexpr (V == 4)
+        *(floatx4*)(in.buf + o) = (floatx4){b.v[0], b.v[1], b.v[2], b.v[3]};
+      else
+        in.buf[o] = b.v[0];
+      u = update_from<V>(in, u, b);
+    }
+#pragma unroll
+    for (int q = 0; q < V; ++q) s += (double)u.v[q] * u.v[q];
+    r += dr;
+    c += dc;
+    if (c >= in.cols) {
+      c -= in.cols;
+      ++r;
+    }
+  }
+  return s;
+}
 __global__ void __launch_bounds__(kInT) k_ns_norm(const Input in, int64_t per, double* part) {
   __shared__ double sh[kInT / 64];
   const int64_t e0 = blockIdx.x * per, e1 = min(in.rows * in.cols, e0 + per);
@@ -390,32 +623,18 @@ __global__ void __launch_bounds__(kInT) k_ns_norm(const Input in, int64_t per, d
     if (!in.clip->finite) return;
     scale = in.clip->scale;
   }
-  double s = 0;
-  const int64_t dr = kInT / in.cols, dc = kInT - dr * in.cols;
-  int64_t r = (e0 + threadIdx.x) / in.cols, c = (e0 + threadIdx.x) - r * in.cols;
-  for (int64_t e = e0 + threadIdx.x; e < e1; e += kInT) {
-    const int64_t o = base + r * in.row_stride + c;
-    if (in.buf) in.buf[o] = fmaf(in.mu, in.buf[o], in.nu * grad_at(in, o, scale));
-    const double u = update_at(in, o, scale);
-    s += u * u;
-    r += dr;
-    c += dc;
-    if (c >= in.cols) {
-      c -= in.cols;
-      ++r;
-    }
-  }
+  double s = in.vec ? norm_chunk<4>(in, e0, e1, base, scale) : norm_chunk<1>(in, e0, e1, base, scale);
   s = wave_sum_d(s);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x == 0) part[blockIdx.y * (int64_t)gridDim.x + blockIdx.x] = (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
-// Block (64-row and 64-column tile of X, matrix): X = u / (|u| + eps) both ways round.
+// Block (64-row and 64-column tile of X, matrix): X = u / (|u| + eps).
 template <bool FLIP>
 __global__ void __launch_bounds__(kInT) k_ns_split(const Input in, const double* part, int nparts,
-                                                   int mp, int np, Mat X, Mat Xt) {
-  __shared__ float tile[64][65];
+                                                   int mp, int np, Mat X) {
+  __shared__ float tile[FLIP ? 64 : 1][65];
   __shared__ double sh[kInT / 64];
   const int bt = blockIdx.y;
   float gs = 1.f;
@@ -432,34 +651,44 @@ __global__ void __launch_bounds__(kInT) k_ns_split(const Input in, const double*
   // a matrix of zeros with eps 0 stays zero
   const double f = norm > 0 ? (double)kScale / norm : (norm == 0 ? 0.0 : norm);
   const int tn = np / 64, ti = blockIdx.x / tn, tj = blockIdx.x - ti * tn;  // tile of X
-  // read along the caller's rows
+  // read along the caller's rows, four elements per thread
   const int64_t r0 = FLIP ? tj * 64 : ti * 64, c0 = FLIP ? ti * 64 : tj * 64;
-  const int lc = threadIdx.x & 63, lr = threadIdx.x >> 6;
-#pragma unroll 4
-  for (int k = 0; k < 16; ++k) {
-    const int64_t r = r0 + k * 4 + lr, c = c0 + lc;
-    float x = 0.f;
-    if (r < in.rows && c < in.cols)
-      x = (float)(update_at(in, bt * in.batch_stride + r * in.row_stride + c, gs) * f);
-    if (FLIP) tile[lc][k * 4 + lr] = x; else tile[k * 4 + lr][lc] = x;
-  }
-  __syncthreads();
+  const int c4 = (threadIdx.x & 15) * 4, lr = threadIdx.x >> 4;
+  floatx4 x[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const int e = k * kInT + threadIdx.x, row = e >> 4, c4 = (e & 15) * 4;
-    floatx4 x, y;
+    const int64_t r = r0 + k * 16 + lr, c = c0 + c4;
+    const int64_t o = bt * in.batch_stride + r * in.row_stride + c;
+    x[k] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    if (in.vec) {
+      if (r < in.rows && c < in.cols) {
+        const Vals<4> u = update_at<4>(in, o, gs);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      x[q] = tile[row][c4 + q];
-      y[q] = tile[c4 + q][row];
+        for (int q = 0; q < 4; ++q) x[k][q] = (float)(u.v[q] * f);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (r < in.rows && c + q < in.cols) x[k][q] = (float)(update_at<1>(in, o + q, gs).v[0] * f);
     }
-    const int64_t o = bt * X.step + blk_at(ti * 64 + row, tj * 64 + c4, np);
-    const int64_t ot = bt * Xt.step + blk_at(tj * 64 + row, ti * 64 + c4, mp);
-    const f16x4 hx = hi_of(x), hy = hi_of(y);
-    *(f16x4*)(X.hi + o) = hx;
-    *(f16x4*)(X.lo + o) = lo_of(x, hx);
-    *(f16x4*)(Xt.hi + ot) = hy;
-    if (Xt.lo) *(f16x4*)(Xt.lo + ot) = lo_of(y, hy);
+  }
+  if (FLIP) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tile[c4 + q][k * 16 + lr] = x[k][q];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[k][q] = tile[k * 16 + lr][c4 + q];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int64_t o = bt * X.step + blk_at(ti * 64 + k * 16 + lr, tj * 64 + c4, np);
+    const f16x4 h = hi_of(x[k]);
+    *(f16x4*)(X.hi + o) = h;
+    *(f16x4*)(X.lo + o) = lo_of(x[k], h);
   }
 }
 
@@ -487,7 +716,7 @@ Plan plan(const rft_matrices& x, const rft_muon_params& p, int out_dtype) {
 }
 
 struct Ws {
-  Mat X, Xt[2], O, P;
+  Mat X[2], O, P;
   float *d, *p;
   double* part;
   size_t bytes;
@@ -502,9 +731,8 @@ Ws carve(void* base, const Plan& q) {
     m.lo = lo ? c.take<_Float16>((size_t)(step * q.batch)) : nullptr;
     return m;
   };
-  w.X = mat(q.mp * q.np, true);
-  w.Xt[0] = mat(q.mp * q.np, q.three);
-  w.Xt[1] = mat(q.mp * q.np, q.three);
+  w.X[0] = mat(q.mp * q.np, true);
+  w.X[1] = mat(q.mp * q.np, true);
   w.O = mat(q.mp * q.mp, q.three);
   w.P = mat(q.mp * q.mp, q.three);
   w.d = c.take<float>((size_t)(q.mp * q.batch));
@@ -514,14 +742,37 @@ Ws carve(void* base, const Plan& q) {
   return w;
 }
 
+// Tile side in panels for C of pm x pn panels (sym: its upper triangle).  A round of 256
+// tiles of 256 x 256 takes as long as four of 128 x 128 or longer, as far as both are
+// bound by the matrix instructions.
+int tile_of(const Plan& q, int64_t pm, int64_t pn, bool sym) {
+  auto tiles = [&](int64_t t) {
+    const int64_t m = (pm + t - 1) / t, n = (pn + t - 1) / t;
+    return (sym ? m * (m + 1) / 2 : m * n) * q.batch;
+  };
+  return tiles(2) >= 512 ? 2 : 1;
+}
+
 template <int EPI, bool FLIP = false>
-hipError_t product(const Plan& q, const Args& g, hipStream_t s) {
+hipError_t product(const Plan& q, Args& g, hipStream_t s) {
+  const int t = tile_of(q, g.pa, g.pb, g.sym);
+  g.tm = (g.pa + t - 1) / t;
+  g.tn = (g.pb + t - 1) / t;
   const int64_t tiles = g.sym ? (int64_t)g.tm * (g.tm + 1) / 2 : (int64_t)g.tm * g.tn;
   const dim3 grid((unsigned)tiles, (unsigned)q.batch);
+  auto go = [&](auto prod) {
+    constexpr int P = decltype(prod)::value;
+    if (t == 2)
+      k_ns<P, EPI, FLIP, 2, 2><<<grid, NT, 0, s>>>(g);
+    else if (tiles * q.batch <= 256)
+      k_ns<P, EPI, FLIP, 1, 4><<<grid, NT, 0, s>>>(g);
+    else
+      k_ns<P, EPI, FLIP, 1, 2><<<grid, NT, 0, s>>>(g);
+  };
   if (q.three)
-    k_ns<3, EPI, FLIP><<<grid, NT, 0, s>>>(g);
+    go(std::integral_constant<int, 3>{});
   else
-    k_ns<1, EPI, FLIP><<<grid, NT, 0, s>>>(g);
+    go(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
 
@@ -532,12 +783,11 @@ hipError_t orthogonalize(const Plan& q, const Input& in, const Result& res,
   if ((e = hipGetLastError())) return e;
   const dim3 tiles((unsigned)((q.mp / 64) * (q.np / 64)), (unsigned)q.batch);
   if (q.flip)
-    k_ns_split<true><<<tiles, kInT, 0, s>>>(in, w.part, (int)q.nparts, (int)q.mp, (int)q.np, w.X, w.Xt[0]);
+    k_ns_split<true><<<tiles, kInT, 0, s>>>(in, w.part, (int)q.nparts, (int)q.mp, (int)q.np, w.X[0]);
   else
-    k_ns_split<false><<<tiles, kInT, 0, s>>>(in, w.part, (int)q.nparts, (int)q.mp, (int)q.np, w.X, w.Xt[0]);
+    k_ns_split<false><<<tiles, kInT, 0, s>>>(in, w.part, (int)q.nparts, (int)q.mp, (int)q.np, w.X[0]);
   if ((e = hipGetLastError())) return e;
   Args g = {};
-  g.X = w.X;
   g.O = w.O;
   g.P = w.P;
   g.d = w.d;
@@ -548,20 +798,21 @@ hipError_t orthogonalize(const Plan& q, const Input& in, const Result& res,
   g.b = (float)p.b;
   g.c = (float)p.c;
   g.r = res;
-  const int tm = (int)(q.mp / 128), tn = (int)(q.np / 128);
+  const int pm = (int)(q.mp / 128), pn = (int)(q.np / 128);
   for (int i = 0; i < p.steps; ++i) {
-    g.A = g.B = w.X;
+    g.X = w.X[i & 1];
+    g.Y = w.X[(i + 1) & 1];
+    g.A = g.B = g.X;
     g.K = (int)q.np;
-    g.tm = g.tn = tm;
+    g.pa = g.pb = pm;
     g.sym = 1;
     if ((e = product<GRAM>(q, g, s))) return e;
     g.A = g.B = w.O;
     g.K = (int)q.mp;
     if ((e = product<POLY>(q, g, s))) return e;
     g.A = w.P;
-    g.B = w.Xt[i & 1];
-    g.Xt = w.Xt[(i + 1) & 1];
-    g.tn = tn;
+    g.B = g.X;
+    g.pb = pn;
     g.sym = 0;
     e = i + 1 < p.steps ? product<APPLY>(q, g, s)
         : q.flip        ? product<LAST, true>(q, g, s)
@@ -574,6 +825,13 @@ hipError_t orthogonalize(const Plan& q, const Input& in, const Result& res,
 }  // namespace ns
 
 namespace {
+
+// Whether the arrays (bytes per element: 2 or 4) can be taken four elements of a row at a time.
+bool by_four(const rft_matrices& x, const void* p, int bytes) {
+  return !p || (x.cols % 4 == 0 && (x.rows == 1 || x.row_stride % 4 == 0) &&
+                (x.batch <= 1 || x.batch_stride % 4 == 0) && (uintptr_t)p % (4 * bytes) == 0);
+}
+int bytes_of(int dtype) { return dtype == RFT_BF16 ? 2 : 4; }
 
 // Finite also as a float.
 bool fits(double x) { return std::fabs(x) <= 1e30; }
@@ -635,7 +893,8 @@ rft_status rft_orthogonalize(const rft_matrices* mats, const void* g, int dtype,
   ns::Ws w = ns::carve(nullptr, q);
   if ((st = check_ws(fn, ws, ws_bytes, w.bytes))) return st;
   w = ns::carve(ws, q);
-  ns::Input in = {mats->rows, mats->cols, mats->row_stride, mats->batch_stride, g, dtype == RFT_BF16,
+  ns::Input in = {mats->rows, mats->cols, mats->row_stride, mats->batch_stride,
+                  by_four(*mats, g, bytes_of(dtype)), g, dtype == RFT_BF16,
                   nullptr, 0.f, 1.f, 0, nullptr, params->eps};
   ns::Result r = {};
   r.flip = q.flip;
@@ -644,6 +903,7 @@ rft_status rft_orthogonalize(const rft_matrices* mats, const void* g, int dtype,
   r.row_stride = mats->row_stride;
   r.batch_stride = mats->batch_stride;
   r.out = out;
+  r.vec = by_four(*mats, out, bytes_of(out_dtype));
   r.out_bf16 = out_dtype == RFT_BF16;
   r.scale = (float)params->scale;
   RFT_HIP(ns::orthogonalize(q, in, r, *params, w, (hipStream_t)stream), fn);
@@ -672,7 +932,8 @@ rft_status rft_muon_step(const rft_matrices* mats, const void* grad, int grad_dt
   ns::Ws w = ns::carve(nullptr, q);
   if ((st = check_ws(fn, ws, ws_bytes, w.bytes))) return st;
   w = ns::carve(ws, q);
-  ns::Input in = {mats->rows, mats->cols, mats->row_stride, mats->batch_stride, grad,
+  ns::Input in = {mats->rows, mats->cols, mats->row_stride, mats->batch_stride,
+                  by_four(*mats, grad, bytes_of(grad_dtype)) && by_four(*mats, momentum_buf, 4), grad,
                   grad_dtype == RFT_BF16, momentum_buf, (float)params->momentum,
                   (float)(1.0 - params->momentum), params->nesterov != 0, clip, params->eps};
   ns::Result r = {};
@@ -682,6 +943,7 @@ rft_status rft_muon_step(const rft_matrices* mats, const void* grad, int grad_dt
   r.row_stride = mats->row_stride;
   r.batch_stride = mats->batch_stride;
   r.weight = weight;
+  r.vec = by_four(*mats, weight, bytes_of(weight_dtype)) && by_four(*mats, master, 4);
   r.weight_bf16 = weight_dtype == RFT_BF16;
   r.master = master;
   r.decay = (float)(1.0 - params->lr * params->weight_decay);
