@@ -87,12 +87,16 @@ struct Args {
   Result r;
 };
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const void* p, int bytes) {
+// Buffer descriptor (wave-uniform) over `bytes` bytes from p.
+struct Desc {
+  uint64_t p;
+  int bytes;
+};
+__device__ __forceinline__ Desc desc(const void* p, int bytes) {
   const uint64_t a = (uint64_t)p;
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
   const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
-  return __builtin_amdgcn_make_buffer_rsrc((void*)(((uint64_t)hi << 32) | lo), 0,
-                                           __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+  return {((uint64_t)hi << 32) | lo, __builtin_amdgcn_readfirstlane(bytes)};
 }
 __device__ __forceinline__ void barrier_lds() {
   asm volatile("" ::: "memory");
@@ -112,6 +116,29 @@ __device__ __forceinline__ floatx4 join(const _Float16* p) {
 // lane s of a group reads columns 4 (s % 4) .. of row s / 4 of its own.
 __device__ __forceinline__ s16x4 read_tr(const char* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+}
+
+// 16 bytes per lane from d (offset v + s) to LDS at dst + 16 lane.  In the kernels that read
+// LDS transposed the compiler waits for every such load before each of those reads (not
+// before others), so there the instruction is written out; it has no register result, and the
+// kernels' own waits cover it.
+template <bool ASM>
+__device__ __forceinline__ void load_lds(const Desc& d, char* dst, uint32_t v, int s) {
+#ifdef __HIP_DEVICE_COMPILE__
+  if constexpr (ASM) {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4 w = {(uint32_t)d.p, (uint32_t)(d.p >> 32) & 0xffffu, (uint32_t)d.bytes, 0x00020000u};
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)dst);
+    // five wait states: scalar registers that a vector instruction has just written
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(at), "v"(v), "s"(w), "s"(s)
+                 : "memory", "m0");
+  } else {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        __builtin_amdgcn_make_buffer_rsrc((void*)d.p, 0, d.bytes, 0x00020000), (lds_ptr)dst, 16, v, s, 0, 0);
+  }
+#endif
 }
 
 // s_waitcnt vmcnt(N), the other counters left alone.
@@ -160,13 +187,13 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   const int panel = g.K * 256;                       // bytes of a panel of A (and of B)
   const int64_t oA = bt * g.A.step + (int64_t)ti * TP * (panel / 2);
   const int nA = min(TP, g.pa - ti * TP) * panel;
-  const __amdgpu_buffer_rsrc_t rA = rsrc(g.A.hi + oA, nA);
-  const __amdgpu_buffer_rsrc_t rAl = rsrc((NOP == 2 ? g.A.lo : g.A.hi) + oA, nA);
+  const Desc rA = desc(g.A.hi + oA, nA);
+  const Desc rAl = desc((NOP == 2 ? g.A.lo : g.A.hi) + oA, nA);
   const int rowsB = TR ? g.np * 256 : panel;         // bytes of 128 rows of B
   const int64_t oB = bt * g.B.step + (TR ? 0 : (int64_t)tj * TP * (panel / 2));
   const int nB = TR ? rowsB : min(TP, g.pb - tj * TP) * panel;
-  const __amdgpu_buffer_rsrc_t rB = rsrc(g.B.hi + oB, nB);
-  const __amdgpu_buffer_rsrc_t rBl = rsrc((NOP == 2 ? g.B.lo : g.B.hi) + oB, nB);
+  const Desc rB = desc(g.B.hi + oB, nB);
+  const Desc rBl = desc((NOP == 2 ? g.B.lo : g.B.hi) + oB, nB);
   // LDS rows of 64 bytes.  Read along the rows (a 16-byte chunk of 16 rows by each of four
   // lane groups): chunk c of row r lies at c ^ key((r >> 2) & 3), key 0 2 3 1, with which the
   // lanes that ds_read_b128 serves together (0-3, 12-15, 20-23, 24-27, then 4-11, 16-19,
@@ -181,19 +208,17 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   // What may pass a descriptor's end goes into the vector part of the offset, which is what
   // the hardware compares; a stage past the last reads zeros (off = 2^31), so that the loop
   // has no branches.
-  auto load_row = [&](__amdgpu_buffer_rsrc_t r, char* dst, int kt, uint32_t off, int p) {
+  auto load_row = [&](const Desc& r, char* dst, int kt, uint32_t off, int p) {
     const int q = wid * NI + p, kb = q / (8 * TP), pn = (q >> 3) % TP, part = q & 7;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        r, (lds_ptr)(dst + q * 1024), 16,
-        vr + ((uint32_t)(pn * panel + kb * kBlkBytes + part * 1024) | off), kt * KB * kBlkBytes, 0, 0);
+    load_lds<TR>(r, dst + q * 1024,
+                 vr + ((uint32_t)(pn * panel + kb * kBlkBytes + part * 1024) | off), kt * KB * kBlkBytes);
   };
   // 32 rows (from 32 kt KB on) x 128 TP columns: 4 TP blocks' 2 KiB pieces
-  auto load_col = [&](__amdgpu_buffer_rsrc_t r, char* dst, int kt, uint32_t off, int p) {
+  auto load_col = [&](const Desc& r, char* dst, int kt, uint32_t off, int p) {
     const int q = wid * NI + p, kb = q / (8 * TP), cb = (q >> 1) % (4 * TP), half = q & 1;
     const int k0 = (kt * KB & 3) * 32;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        r, (lds_ptr)(dst + q * 1024), 16,
-        vt + ((uint32_t)((tj * 4 * TP + cb) * kBlkBytes + kb * 2048 + half * 1024) | off), k0 * 64, 0, 0);
+    load_lds<TR>(r, dst + q * 1024,
+                 vt + ((uint32_t)((tj * 4 * TP + cb) * kBlkBytes + kb * 2048 + half * 1024) | off), k0 * 64);
   };
   const int nk = g.K / (BC * KB);  // K is a multiple of 128: nk is even where KB = 1
   constexpr int L = 2 * NOP * NI;  // load instructions per wave and stage
@@ -207,7 +232,7 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
       load_row(lo ? rAl : rA, d, kt, off, p);
     } else if (TR) {
       const int64_t o = oB + (int64_t)(kt * KB >> 2) * (rowsB / 2);
-      load_col(rsrc((lo ? g.B.lo : g.B.hi) + o, rowsB), d, kt, off, p);
+      load_col(desc((lo ? g.B.lo : g.B.hi) + o, rowsB), d, kt, off, p);
     } else {
       load_row(lo ? rBl : rB, d, kt, off, p);
     }
