@@ -118,6 +118,50 @@ __device__ __forceinline__ s16x4 read_tr(const char* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
 
+// The weights' four elements at `at`, where four can be taken at a time.
+__device__ __forceinline__ floatx4 weights_at(const Result& r, int64_t at) {
+  if (r.master) return *(const floatx4*)(r.master + at);
+  if (!r.weight_bf16) return *(const floatx4*)((const float*)r.weight + at);
+  const u16x4 h = *(const u16x4*)((const uint16_t*)r.weight + at);
+  return (floatx4){bf16_to_f32(h[0]), bf16_to_f32(h[1]), bf16_to_f32(h[2]), bf16_to_f32(h[3])};
+}
+// The result y (scaled) of elements [v, v + 4) of a row that ends at `end`, at `at`; w: the
+// weights there (r.vec, which implies that the row's length is a multiple of four).
+__device__ __forceinline__ void result_at(const Result& r, int64_t at, int64_t v, int64_t end,
+                                          floatx4 y, floatx4 w) {
+  if (v >= end) return;
+  void* const dst = r.weight ? r.weight : r.out;
+  const bool half = r.weight ? r.weight_bf16 : r.out_bf16;
+  if (r.vec) {
+    if (r.weight) {
+      y = w * r.decay - y;
+      if (r.master) *(floatx4*)(r.master + at) = y;
+    }
+    if (half)
+      *(u16x4*)((uint16_t*)dst + at) = (u16x4){f32_to_bf16(y[0]), f32_to_bf16(y[1]),
+                                               f32_to_bf16(y[2]), f32_to_bf16(y[3])};
+    else
+      *(floatx4*)((float*)dst + at) = y;
+    return;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (v + q >= end) continue;
+    float z = y[q];
+    if (r.weight) {
+      const float w0 = r.master ? r.master[at + q]
+                       : r.weight_bf16 ? bf16_to_f32(((const uint16_t*)r.weight)[at + q])
+                                       : ((const float*)r.weight)[at + q];
+      z = w0 * r.decay - z;
+      if (r.master) r.master[at + q] = z;
+    }
+    if (half)
+      ((uint16_t*)dst)[at + q] = f32_to_bf16(z);
+    else
+      ((float*)dst)[at + q] = z;
+  }
+}
+
 // 16 bytes per lane from d (offset v + s) to LDS at dst + 16 lane.  In the kernels that read
 // LDS transposed the compiler waits for every such load before each of those reads (not
 // before others), so there the instruction is written out; it has no register result, and the
@@ -380,15 +424,7 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
     auto old = [&](int i, int j) {  // the weights' tile, where four can be taken at a time
       int64_t v;
       const int64_t at = place(i, j, v);
-      if (!r.weight || !r.vec || j0 + j * 16 >= g.np || v >= end) return;
-      if (r.master) {
-        w[j] = *(const floatx4*)(r.master + at);
-      } else if (r.weight_bf16) {
-        const u16x4 h = *(const u16x4*)((const uint16_t*)r.weight + at);
-        w[j] = (floatx4){bf16_to_f32(h[0]), bf16_to_f32(h[1]), bf16_to_f32(h[2]), bf16_to_f32(h[3])};
-      } else {
-        w[j] = *(const floatx4*)((const float*)r.weight + at);
-      }
+      if (r.weight && r.vec && j0 + j * 16 < g.np && v < end) w[j] = weights_at(r, at);
     };
     if (SB == 2) state(0, 0);
 #pragma unroll
@@ -415,38 +451,8 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
         }
         int64_t v;
         const int64_t at = place(i, j, v);
-        if (v >= end) continue;
         if (SB == 1) old(i, j);
-        void* const dst = r.weight ? r.weight : r.out;
-        const bool half = r.weight ? r.weight_bf16 : r.out_bf16;
-        if (r.vec) {
-          if (r.weight) {
-            y = w[j] * r.decay - y;
-            if (r.master) *(floatx4*)(r.master + at) = y;
-          }
-          if (half)
-            *(u16x4*)((uint16_t*)dst + at) = (u16x4){f32_to_bf16(y[0]), f32_to_bf16(y[1]),
-                                                     f32_to_bf16(y[2]), f32_to_bf16(y[3])};
-          else
-            *(floatx4*)((float*)dst + at) = y;
-          continue;
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (v + q >= end) continue;
-          float z = y[q];
-          if (r.weight) {
-            const float w0 = r.master ? r.master[at + q]
-                             : r.weight_bf16 ? bf16_to_f32(((const uint16_t*)r.weight)[at + q])
-                                             : ((const float*)r.weight)[at + q];
-            z = w0 * r.decay - z;
-            if (r.master) r.master[at + q] = z;
-          }
-          if (half)
-            ((uint16_t*)dst)[at + q] = f32_to_bf16(z);
-          else
-            ((float*)dst)[at + q] = z;
-        }
+        result_at(r, at, v, end, y, w[j]);
       }
     }
   } else {
@@ -538,6 +544,267 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
         }
       }
     }
+  }
+}
+
+// ------------------------------------------------------- up to 128 rows --
+// Matrices whose shorter side is at most 128: A, its polynomial and the products with X fit
+// one workgroup, and what the three kernels above spend on such matrices is launches and
+// latencies (12, 6 and 8 us per step at 128 x 1536).  A workgroup owns `per` slabs of 128
+// columns of X.  A step of a slab takes P X, the new X and its part of X X^T (64 KiB of X in
+// LDS); A and P are formed by every workgroup of a matrix for itself, from the parts of A
+// that the last launch left (the end of a launch is what orders the workgroups).  A matrix
+// with one workgroup runs all its steps in one launch.
+struct SmallArgs {
+  Mat X[2];      // ping-pong
+  float* part;   // [batch][2][groups][128 x 128] parts of A, by lane
+  int np, groups, per;
+  int it0, it1, steps;  // steps of this launch; it0 == it1: the parts of A of X[0]
+  float a, b, c;
+  Result r;
+};
+
+template <int PROD, bool FLIP>
+__global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
+  constexpr int NOP = PROD == 3 ? 2 : 1;
+  constexpr int OP = 4 * kBlkBytes;  // bytes of a 128 x 128 plane
+  __shared__ __attribute__((aligned(16))) char lds[(NOP + 2) * OP];
+  __shared__ __attribute__((aligned(16))) float sd[128], sp[128];
+  char* const op = lds;             // O, then P: planes hi, lo
+  char* const xb = lds + NOP * OP;  // a slab of X: planes hi, lo
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wid >> 2, wn = wid & 3;  // waves of 64 x 32
+  const int r16 = lane & 15, q4 = lane >> 4;
+  const int grp = blockIdx.x, bt = blockIdx.y;
+  const int s0 = grp * g.per, s1 = min(g.np / 128, s0 + g.per);
+  auto key = [](int x) { return (0x78 >> (2 * (x & 3))) & 3; };
+  // lane parts of the loads and fragment reads: as in k_ns
+  const uint32_t vr = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ key(lane >> 4)) << 4));
+  const uint32_t vt = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ (((lane >> 5) & 1) << 1)) << 4));
+  const int cr = (q4 ^ key(r16 >> 2)) << 4;
+  const int rt = 8 * q4 + (r16 >> 2), ct0 = (r16 & 3) >> 1, ct1 = (r16 & 1) * 8;
+  // byte of (row, column 32 cb + 16 h + 4 q4) in a plane, with either order of chunks
+  auto at_rows = [&](int row, int cb, int h) {
+    return cb * kBlkBytes + row * 64 + (((h * 2 + (q4 >> 1)) ^ key(row >> 2)) << 4) + (q4 & 1) * 8;
+  };
+  auto at_cols = [&](int row, int cb, int h) {
+    return cb * kBlkBytes + row * 64 + (((h * 2 + (q4 >> 1)) ^ (((row >> 3) & 1) << 1)) << 4) + (q4 & 1) * 8;
+  };
+  auto load_slab = [&](const Mat& x, int slab, uint32_t v, int planes) {
+    for (int o = 0; o < planes; ++o) {
+      const Desc d = desc((o ? x.lo : x.hi) + bt * x.step + (int64_t)slab * 4 * kBlk, OP);
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const int q = wid * 4 + p;
+        load_lds<false>(d, xb + o * OP + q * 1024, v + (uint32_t)q * 1024u, 0);
+      }
+    }
+  };
+  // acc += A B^T over 128 columns, both row-wise, or (tr) A times the columns of a slab
+  auto products = [&](floatx4 (&acc)[4][2], const char* A, const char* B, auto tr) {
+    constexpr bool TR = decltype(tr)::value;
+#pragma unroll
+    for (int kb = 0; kb < 4; ++kb) {
+      f16x8 a[NOP][4], b[NOP][2];
+#pragma unroll
+      for (int o = 0; o < NOP; ++o) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          a[o][i] = *(const f16x8*)(A + o * OP + kb * kBlkBytes + (wm * 64 + i * 16 + r16) * 64 + cr);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if (TR) {
+            s16x4 h[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              h[u] = read_tr(B + o * OP + wn * kBlkBytes + (kb * 32 + rt + 4 * u) * 64 +
+                             (((j * 2 + ct0) ^ ((q4 & 1) << 1)) << 4) + ct1);
+            b[o][j] = __builtin_bit_cast(
+                f16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+          } else {
+            b[o][j] = *(const f16x8*)(B + o * OP + kb * kBlkBytes + (wn * 32 + j * 16 + r16) * 64 + cr);
+          }
+        }
+      }
+#pragma unroll
+      for (int pr = 0; pr < PROD; ++pr) {
+        const int oa = pr == 2 ? 1 : 0, ob = pr == 1 ? 1 : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[ob][j], a[oa][i], acc[i][j], 0, 0, 0);
+      }
+    }
+  };
+  auto clear = [](floatx4 (&acc)[4][2]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
+  };
+  // hi (and lo) of x at (row, 4 columns) to a pair of planes at `base`
+  auto put = [&](char* base, int where, floatx4 x, bool lo) {
+    const f16x4 h = hi_of(x);
+    *(f16x4*)(base + where) = h;
+    if (lo) *(f16x4*)(base + OP + where) = lo_of(x, h);
+  };
+  auto part_at = [&](int parity, int group) {
+    return g.part + (((int64_t)bt * 2 + parity) * g.groups + group) * 16384 + (wid * 8 * 64 + lane) * 4;
+  };
+  const std::false_type rows{};
+  const std::true_type cols{};
+
+  floatx4 gram[4][2];
+  clear(gram);
+  bool have = false;  // gram holds this matrix's whole A
+  if (g.it0 == 0 && (g.groups == 1 || g.it0 == g.it1)) {
+    for (int s = s0; s < s1; ++s) {
+      load_slab(g.X[0], s, vr, NOP);
+      wait_vm<0>();
+      __syncthreads();
+      products(gram, xb, xb, rows);
+      __syncthreads();  // the slab is read
+    }
+    have = g.groups == 1;
+  }
+  for (int it = g.it0; it < g.it1; ++it) {
+    const Mat& X = g.X[it & 1];
+    const Mat& Y = g.X[(it + 1) & 1];
+    const bool last = it + 1 == g.steps;
+    if (!have) {
+      clear(gram);
+      for (int p = 0; p < g.groups; ++p) {
+        const float* const src = part_at(it & 1, p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) gram[i][j] += *(const floatx4*)(src + (i * 2 + j) * 256);
+      }
+    }
+    load_slab(X, s0, vt, 2);  // arrives behind the polynomial
+    // A = D + O
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int row = wm * 64 + i * 16 + r16, col = wn * 32 + j * 16 + q4 * 4;
+        floatx4 x = gram[i][j] * kInv;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (row == col + q) {
+            sd[row] = x[q] * kInv;
+            x[q] = 0.f;
+          }
+        gram[i][j] = x;
+        put(op, at_rows(row, wn, j), x, NOP == 2);
+      }
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    barrier_lds();  // not __syncthreads: the slab may still be on its way
+    floatx4 acc[4][2];
+    clear(acc);
+    products(acc, op, op, rows);
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    barrier_lds();  // O is read
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = wm * 64 + i * 16 + r16;
+      const float dr = sd[row];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int col = wn * 32 + j * 16 + q4 * 4;
+        const floatx4 dc = *(const floatx4*)(sd + col), s = gram[i][j];
+        floatx4 x = acc[i][j] * kInv;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (row == col + q) {
+            sp[row] = g.a + g.b * dr + g.c * (x[q] * kInv + dr * dr);
+            x[q] = 0.f;
+          } else {
+            x[q] = g.b * s[q] + g.c * (x[q] + (dr + dc[q]) * s[q]);
+          }
+        }
+        put(op, at_rows(row, wn, j), x, NOP == 2);
+      }
+    }
+    clear(gram);
+    for (int s = s0; s < s1; ++s) {
+      wait_vm<0>();
+      __syncthreads();  // P and the slab are there
+      clear(acc);
+      products(acc, op, xb, cols);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = wm * 64 + i * 16 + r16;
+        const float pr = sp[row];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const char* const x = xb + at_cols(row, wn, j);
+          const floatx4 st = join((const _Float16*)x) + join((const _Float16*)(x + OP));
+          acc[i][j] = acc[i][j] * kInv + pr * st;
+        }
+      }
+      __syncthreads();  // the slab is read
+      if (!last) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int row = wm * 64 + i * 16 + r16, col = s * 128 + wn * 32 + j * 16 + q4 * 4;
+            const int64_t o = bt * Y.step + blk_at(row, col, g.np);
+            const f16x4 h = hi_of(acc[i][j]), l = lo_of(acc[i][j], h);
+            *(f16x4*)(Y.hi + o) = h;
+            *(f16x4*)(Y.lo + o) = l;
+            char* const x = xb + at_rows(row, wn, j);
+            *(f16x4*)x = h;
+            if (NOP == 2) *(f16x4*)(x + OP) = l;
+          }
+        __syncthreads();
+        products(gram, xb, xb, rows);
+      } else if (!g.r.clip || g.r.clip->finite) {
+        const Result& r = g.r;
+        const int64_t M = r.flip ? r.cols : r.rows, N = r.flip ? r.rows : r.cols;
+        const int64_t end = FLIP ? M : N;
+        const float f = kInv * r.scale;
+        float* const t = (float*)(xb + wid * 2048);  // of this wave
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            floatx4 y = acc[i][j] * f;
+            const int r0 = wm * 64 + i * 16, c0 = s * 128 + wn * 32 + j * 16;
+            int64_t u = r0 + r16, v = c0 + q4 * 4;
+            if (FLIP) {
+              __builtin_amdgcn_wave_barrier();
+              *(floatx4*)(t + r16 * 20 + q4 * 4) = y;
+              __builtin_amdgcn_wave_barrier();
+#pragma unroll
+              for (int q = 0; q < 4; ++q) y[q] = t[(q4 * 4 + q) * 20 + r16];
+              u = c0 + r16;
+              v = r0 + q4 * 4;
+            }
+            if (u >= (FLIP ? N : M)) v = end;
+            const int64_t at = bt * r.batch_stride + u * r.row_stride + v;
+            floatx4 w = {0.f, 0.f, 0.f, 0.f};
+            if (r.weight && r.vec && v < end) w = weights_at(r, at);
+            result_at(r, at, v, end, y, w);
+          }
+      }
+      if (s + 1 < s1) {
+        __syncthreads();  // the new slab is read
+        load_slab(X, s + 1, vt, 2);
+      }
+    }
+    have = g.groups == 1;
+    __syncthreads();  // this step's stores, before the next step's loads of them
+  }
+  if (!have && g.it1 < g.steps) {
+    float* const dst = part_at(g.it1 & 1, grp);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) *(floatx4*)(dst + (i * 2 + j) * 256) = gram[i][j];
   }
 }
 
@@ -723,6 +990,7 @@ constexpr int64_t kNormBlocks = 1024;  // partial sums of a matrix at most
 struct Plan {
   bool flip, three;
   int64_t m, n, mp, np, batch, nparts, per;
+  int64_t groups, slabs;  // m <= 128: workgroups per matrix, slabs of 128 columns for each
 };
 Plan plan(const rft_matrices& x, const rft_muon_params& p, int out_dtype) {
   Plan q;
@@ -737,12 +1005,24 @@ Plan plan(const rft_matrices& x, const rft_muon_params& p, int out_dtype) {
   const int64_t size = q.m * q.n;
   q.per = round_up((size + kNormBlocks - 1) / kNormBlocks, 4096);
   q.nparts = (size + q.per - 1) / q.per;
+  // k_ns_small: up to three slabs in one workgroup (all steps in one launch); else a slab
+  // takes about five times as long as adding another workgroup's part of A, which makes
+  // sqrt(5 slabs) workgroups the shortest step.  Not by the batch: a matrix gives the same
+  // bits alone and in a stack.
+  q.groups = q.slabs = 0;
+  if (q.mp == 128) {
+    const int64_t n = q.np / 128;
+    const int64_t want = n <= 3 ? 1 : std::min<int64_t>(n, (int64_t)std::ceil(std::sqrt(5.0 * n)));
+    q.slabs = (n + want - 1) / want;
+    q.groups = (n + q.slabs - 1) / q.slabs;
+  }
   return q;
 }
 
 struct Ws {
   Mat X[2], O, P;
   float *d, *p;
+  float* A;  // k_ns_small: parts of A
   double* part;
   size_t bytes;
 };
@@ -758,10 +1038,16 @@ Ws carve(void* base, const Plan& q) {
   };
   w.X[0] = mat(q.mp * q.np, true);
   w.X[1] = mat(q.mp * q.np, true);
-  w.O = mat(q.mp * q.mp, q.three);
-  w.P = mat(q.mp * q.mp, q.three);
-  w.d = c.take<float>((size_t)(q.mp * q.batch));
-  w.p = c.take<float>((size_t)(q.mp * q.batch));
+  w.O = w.P = {};
+  w.d = w.p = w.A = nullptr;
+  if (q.groups) {
+    w.A = c.take<float>((size_t)(q.batch * 2 * q.groups * 16384));
+  } else {
+    w.O = mat(q.mp * q.mp, q.three);
+    w.P = mat(q.mp * q.mp, q.three);
+    w.d = c.take<float>((size_t)(q.mp * q.batch));
+    w.p = c.take<float>((size_t)(q.mp * q.batch));
+  }
   w.part = c.take<double>((size_t)(q.nparts * q.batch));
   w.bytes = c.bytes();
   return w;
@@ -801,6 +1087,24 @@ hipError_t product(const Plan& q, Args& g, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int PROD>
+hipError_t small_steps(const Plan& q, SmallArgs g, hipStream_t s) {
+  const dim3 grid((unsigned)q.groups, (unsigned)q.batch);
+  auto go = [&](int it0, int it1) {
+    g.it0 = it0;
+    g.it1 = it1;
+    if (q.flip)
+      k_ns_small<PROD, true><<<grid, NT, 0, s>>>(g);
+    else
+      k_ns_small<PROD, false><<<grid, NT, 0, s>>>(g);
+    return hipGetLastError();
+  };
+  if (q.groups == 1) return go(0, g.steps);
+  hipError_t e = go(0, 0);
+  for (int i = 0; i < g.steps && !e; ++i) e = go(i, i + 1);
+  return e;
+}
+
 hipError_t orthogonalize(const Plan& q, const Input& in, const Result& res,
                          const rft_muon_params& p, const Ws& w, hipStream_t s) {
   hipError_t e;
@@ -812,6 +1116,21 @@ hipError_t orthogonalize(const Plan& q, const Input& in, const Result& res,
   else
     k_ns_split<false><<<tiles, kInT, 0, s>>>(in, w.part, (int)q.nparts, (int)q.mp, (int)q.np, w.X[0]);
   if ((e = hipGetLastError())) return e;
+  if (q.groups) {
+    SmallArgs a = {};
+    a.X[0] = w.X[0];
+    a.X[1] = w.X[1];
+    a.part = w.A;
+    a.np = (int)q.np;
+    a.groups = (int)q.groups;
+    a.per = (int)q.slabs;
+    a.steps = p.steps;
+    a.a = (float)p.a;
+    a.b = (float)p.b;
+    a.c = (float)p.c;
+    a.r = res;
+    return q.three ? small_steps<3>(q, a, s) : small_steps<1>(q, a, s);
+  }
   Args g = {};
   g.O = w.O;
   g.P = w.P;

@@ -51,7 +51,8 @@ def off(x, ref):
 # an error spread over all directions, of which the small ones hold a part) are taken whole:
 LIMIT = {R.RFT_PRODUCTS_THREE: 2.0 ** -22 * 141, R.RFT_PRODUCTS_ONE: 2.0 ** -11 * 11.9}
 SHAPES = [(1, 1), (1, 7), (5, 1), (2, 3), (16, 16), (17, 90), (64, 64), (63, 129), (128, 128),
-          (129, 128), (128, 300), (200, 70), (257, 256), (384, 640), (1000, 130), (33, 2050)]
+          (129, 128), (128, 300), (200, 70), (257, 256), (384, 640), (1000, 130), (33, 2050), (128, 385),
+          (120, 512), (4000, 100), (3, 9000)]
 
 
 @pytest.mark.parametrize("products", [R.RFT_PRODUCTS_ONE, R.RFT_PRODUCTS_THREE])
@@ -77,7 +78,8 @@ def test_products_by_type():
         assert torch.equal(a, b)
 
 
-@pytest.mark.parametrize("shape", [(3, 40, 200), (5, 130, 60), (7, 1, 9), (2, 256, 256)])
+@pytest.mark.parametrize("shape", [(3, 40, 200), (5, 130, 60), (7, 1, 9), (2, 256, 256), (20, 128, 1700),
+                                   (3, 700, 33), (130, 50, 600)])
 def test_stacks_and_strides(shape):
     b, m, n = shape
     x = matrix(b, *shape)
