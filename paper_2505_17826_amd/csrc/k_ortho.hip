@@ -108,8 +108,38 @@ __device__ __forceinline__ f16x4 hi_of(floatx4 x) { return __builtin_convertvect
 __device__ __forceinline__ f16x4 lo_of(floatx4 x, f16x4 h) {
   return __builtin_convertvector(x - __builtin_convertvector(h, floatx4), f16x4);
 }
-__device__ __forceinline__ floatx4 join(const _Float16* p) {
-  return __builtin_convertvector(*(const f16x4*)p, floatx4);
+
+// A lane's results of two neighbouring 16-column tiles, a (columns 4 q4 .. of a row) and b
+// (16 + 4 q4 ..), as eight consecutive columns 8 q4 .. of the 32, and back: by rows of 16
+// lanes a0 a1 a2 a3 | b0 b1 b2 b3 <-> a0 a2 b0 b2 | a1 a3 b1 b3.  A wave then reads or
+// writes 16 rows of a block, 1 KiB in one piece, with 16 bytes per lane; 8 bytes per lane in
+// pieces of 32 took twice as long.
+__device__ __forceinline__ void swap_words(floatx4& a, floatx4& b, bool upper) {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const uint32_t x = __float_as_uint(a[q]), y = __float_as_uint(b[q]);
+    const auto r = upper ? __builtin_amdgcn_permlane32_swap(x, y, false, false)
+                         : __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    a[q] = __uint_as_float(r[0]);
+    b[q] = __uint_as_float(r[1]);
+  }
+#endif
+}
+__device__ __forceinline__ void widen(floatx4& a, floatx4& b) {
+  swap_words(a, b, true);
+  swap_words(a, b, false);
+}
+__device__ __forceinline__ void narrow(floatx4& a, floatx4& b) {
+  swap_words(a, b, false);
+  swap_words(a, b, true);
+}
+__device__ __forceinline__ floatx4 wide(f16x8 x, int half) {
+  return half ? (floatx4){(float)x[4], (float)x[5], (float)x[6], (float)x[7]}
+              : (floatx4){(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+}
+__device__ __forceinline__ f16x8 both(f16x4 a, f16x4 b) {
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // Four rows (4 g .. of lane group g) of column lane % 16 from a 16-lane group's rows at p:
@@ -389,7 +419,7 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   // ------------------------------------------------------------------ epilogue
   // element q of tile (i, j): row i0 + 16 i + r16, column j0 + 16 j + 4 q4 + q
   const int i0 = (ti * TP + (wm >> 1)) * 128 + (wm & 1) * 64, j0 = tj * TP * 128 + wn * 16 * WN;
-  char* const mine = lds + wid * 2048;  // of this wave: a 16 x 16 tile at a time
+  char* const mine = lds + wid * 2048;  // of this wave: a tile or two at a time
   if (i0 >= g.mp) return;
   // What a row of tiles needs from memory is loaded whole, that of the next row before this
   // one's results are stored (one load at a time, in order with the stores, took
@@ -400,18 +430,19 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
     const int64_t M = r.flip ? r.cols : r.rows, N = r.flip ? r.rows : r.cols;
     const int64_t end = FLIP ? M : N;
     const float f = kInv * r.scale;
-    f16x4 sh[SB][WN], sl[SB][WN];
+    constexpr int WP = WN / 2;
+    f16x8 sh[SB][WP], sl[SB][WP];  // columns j0 + 32 j + 8 q4 ..
     float pi[SB];
     floatx4 w[WN];
     auto state = [&](int i, int to) {
       const int row = i0 + i * 16 + r16;
       pi[to] = g.p[(int64_t)bt * g.mp + row];
 #pragma unroll
-      for (int j = 0; j < WN; ++j) {
-        if (j0 + j * 16 >= g.np) continue;
-        const int64_t o = bt * g.X.step + blk_at(row, j0 + j * 16 + q4 * 4, g.np);
-        sh[to][j] = *(const f16x4*)(g.X.hi + o);
-        sl[to][j] = *(const f16x4*)(g.X.lo + o);
+      for (int j = 0; j < WP; ++j) {
+        if (j0 + j * 32 >= g.np) continue;
+        const int64_t o = bt * g.X.step + blk_at(row, j0 + j * 32 + q4 * 8, g.np);
+        sh[to][j] = *(const f16x8*)(g.X.hi + o);
+        sl[to][j] = *(const f16x8*)(g.X.lo + o);
       }
     };
     // four consecutive elements (u, v) .. of a row of the caller's matrix
@@ -435,12 +466,16 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
         for (int j = 0; j < WN; ++j) old(i, j);
       }
       if (SB == 2 && i + 1 < 4) state(i + 1, (i + 1) & 1);
+      floatx4 x[2];
 #pragma unroll
       for (int j = 0; j < WN; ++j) {
         if (j0 + j * 16 >= g.np) continue;
-        const floatx4 x = __builtin_convertvector(sh[i % SB][j], floatx4) +
-                          __builtin_convertvector(sl[i % SB][j], floatx4);
-        floatx4 y = (pi[i % SB] * x + acc[i][j] * kInv) * f;
+        if (j % 2 == 0) {
+          x[0] = wide(sh[i % SB][j / 2], 0) + wide(sl[i % SB][j / 2], 0);
+          x[1] = wide(sh[i % SB][j / 2], 1) + wide(sl[i % SB][j / 2], 1);
+          narrow(x[0], x[1]);
+        }
+        floatx4 y = (pi[i % SB] * x[j % 2] + acc[i][j] * kInv) * f;
         if (FLIP) {  // the tile transposed through LDS, rows 20 floats apart
           float* const t = (float*)mine;
           __builtin_amdgcn_wave_barrier();
@@ -462,25 +497,28 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
     const int kp = EPI == APPLY ? g.np : g.mp;
     const int64_t vb = (int64_t)bt * g.mp;
     const bool mirror = EPI != APPLY && ti != tj;
-    f16x4 sh[SB][WN], sl[SB][WN];
+    constexpr int WP = WN / 2;  // pairs of tiles: a lane's columns are j0 + 32 j + 8 q4 ..
+    f16x8 sh[SB][WP], sl[SB][WP];
     float di[SB] = {};
     auto state = [&](int i, int to) {
       const int row = i0 + i * 16 + r16;
       if (EPI == POLY) di[to] = g.d[vb + row];
       if (EPI == APPLY) di[to] = g.p[vb + row];
 #pragma unroll
-      for (int j = 0; j < WN; ++j) {
-        if (!HI || j0 + j * 16 >= kp) continue;
-        const int64_t o = bt * src.step + blk_at(row, j0 + j * 16 + q4 * 4, kp);
-        sh[to][j] = *(const f16x4*)(src.hi + o);
-        if (LO) sl[to][j] = *(const f16x4*)(src.lo + o);
+      for (int j = 0; j < WP; ++j) {
+        if (!HI || j0 + j * 32 >= kp) continue;
+        const int64_t o = bt * src.step + blk_at(row, j0 + j * 32 + q4 * 8, kp);
+        sh[to][j] = *(const f16x8*)(src.hi + o);
+        if (LO) sl[to][j] = *(const f16x8*)(src.lo + o);
       }
     };
-    floatx4 dj[WN];
+    floatx4 dj[WP][2];
     if (EPI == POLY && SB == 2) {
 #pragma unroll
-      for (int j = 0; j < WN; ++j)
-        if (j0 + j * 16 < kp) dj[j] = *(const floatx4*)(g.d + vb + j0 + j * 16 + q4 * 4);
+      for (int j = 0; j < WP; ++j)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (j0 + j * 32 < kp) dj[j][e] = *(const floatx4*)(g.d + vb + j0 + j * 32 + q4 * 8 + e * 4);
     }
     if (SB == 2) state(0, 0);
 #pragma unroll
@@ -489,57 +527,66 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
       if (SB == 1) state(i, 0);
       if (SB == 2 && i + 1 < 4) state(i + 1, (i + 1) & 1);
 #pragma unroll
-      for (int j = 0; j < WN; ++j) {
-        const int col = j0 + j * 16 + q4 * 4;
-        if (j0 + j * 16 >= kp) continue;
-        const int64_t o = blk_at(row, col, kp);
-        floatx4 x = acc[i][j] * kInv;  // kScale times the new values
-        floatx4 s = {0.f, 0.f, 0.f, 0.f};
-        if (HI) s = __builtin_convertvector(sh[i % SB][j], floatx4);
-        if (LO) s += __builtin_convertvector(sl[i % SB][j], floatx4);
-        if constexpr (EPI == GRAM) {
+      for (int j = 0; j < WP; ++j) {
+        if (j0 + j * 32 >= kp) continue;
+        const int64_t o = bt * dst.step + blk_at(row, j0 + j * 32 + q4 * 8, kp);
+        const bool on = (i0 + i * 16) >> 5 == (j0 >> 5) + j;  // meets the diagonal
+        widen(acc[i][2 * j], acc[i][2 * j + 1]);
+        f16x4 h[2], l[2];
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (row == col + q) {
-              g.d[vb + row] = x[q] * kInv;
-              x[q] = 0.f;
-            }
-        } else if constexpr (EPI == POLY) {
-          const float dr = di[i % SB];
-          if (SB == 1) dj[j] = *(const floatx4*)(g.d + vb + col);
+        for (int e = 0; e < 2; ++e) {
+          const int col = j0 + j * 32 + q4 * 8 + e * 4;
+          floatx4 x = acc[i][2 * j + e] * kInv;  // kScale times the new values
+          floatx4 s = {0.f, 0.f, 0.f, 0.f};
+          if (HI) s = wide(sh[i % SB][j], e);
+          if (LO) s += wide(sl[i % SB][j], e);
+          if constexpr (EPI == GRAM) {
+            if (on) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            if (row == col + q) {
-              g.p[vb + row] = g.a + g.b * dr + g.c * (x[q] * kInv + dr * dr);
-              x[q] = 0.f;
-            } else {
-              x[q] = g.b * s[q] + g.c * (x[q] + (dr + dj[j][q]) * s[q]);
+              for (int q = 0; q < 4; ++q)
+                if (row == col + q) {
+                  g.d[vb + row] = x[q] * kInv;
+                  x[q] = 0.f;
+                }
             }
+          } else if constexpr (EPI == POLY) {
+            const float dr = di[i % SB];
+            if (SB == 1) dj[j][e] = *(const floatx4*)(g.d + vb + col);
+            floatx4 y;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = g.b * s[q] + g.c * (x[q] + (dr + dj[j][e][q]) * s[q]);
+            if (on) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                if (row == col + q) {
+                  g.p[vb + row] = g.a + g.b * dr + g.c * (x[q] * kInv + dr * dr);
+                  y[q] = 0.f;
+                }
+            }
+            x = y;
+          } else {
+            x += di[i % SB] * s;
           }
-        } else {
-          x += di[i % SB] * s;
+          h[e] = hi_of(x);
+          // lo planes: of X always, of the others where products use them
+          if (EPI == APPLY || NOP == 2) l[e] = lo_of(x, h[e]);
         }
-        const f16x4 h = hi_of(x);
-        *(f16x4*)(dst.hi + bt * dst.step + o) = h;
-        // lo planes: of X always, of the others where products use them
-        f16x4 l;
-        if (EPI == APPLY || NOP == 2) {
-          l = lo_of(x, h);
-          *(f16x4*)(dst.lo + bt * dst.step + o) = l;
-        }
+        *(f16x8*)(dst.hi + o) = both(h[0], h[1]);
+        if (EPI == APPLY || NOP == 2) *(f16x8*)(dst.lo + o) = both(l[0], l[1]);
         if (mirror) {
-          // the 16 x 16 tile through LDS (rows of 32 bytes, read transposed): lane holds
-          // rows 4 q4 .. of column r16, four consecutive elements of the mirrored row
-          const int64_t om = bt * dst.step + blk_at(j0 + j * 16 + r16, i0 + i * 16 + q4 * 4, kp);
+          // 16 rows x 32 columns through LDS (rows of 64 bytes, read transposed): lane holds
+          // rows 4 q4 .. of column 16 e + r16, four consecutive elements of the mirrored row
           __builtin_amdgcn_wave_barrier();
-          *(f16x4*)(mine + r16 * 32 + q4 * 8) = h;
-          if (NOP == 2) *(f16x4*)(mine + 512 + r16 * 32 + q4 * 8) = l;
+          *(f16x8*)(mine + r16 * 64 + q4 * 16) = both(h[0], h[1]);
+          if (NOP == 2) *(f16x8*)(mine + 1024 + r16 * 64 + q4 * 16) = both(l[0], l[1]);
           __builtin_amdgcn_wave_barrier();
-          const s16x4 th = read_tr(mine + lane * 8);
-          *(s16x4*)(dst.hi + om) = th;
-          if (NOP == 2) {
-            const s16x4 tl = read_tr(mine + 512 + lane * 8);
-            *(s16x4*)(dst.lo + om) = tl;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int64_t om =
+                bt * dst.step + blk_at(j0 + j * 32 + e * 16 + r16, i0 + i * 16 + q4 * 4, kp);
+            const char* const t = mine + (q4 * 4 + (r16 >> 2)) * 64 + e * 32 + (r16 & 3) * 8;
+            *(s16x4*)(dst.hi + om) = read_tr(t);
+            if (NOP == 2) *(s16x4*)(dst.lo + om) = read_tr(t + 1024);
           }
         }
       }
@@ -568,10 +615,14 @@ template <int PROD, bool FLIP>
 __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
   constexpr int NOP = PROD == 3 ? 2 : 1;
   constexpr int OP = 4 * kBlkBytes;  // bytes of a 128 x 128 plane
-  __shared__ __attribute__((aligned(16))) char lds[(NOP + 2) * OP];
+  // with one plane per operand the new X has a plane of its own, and the next slab arrives
+  // behind the product with it; with two there is no room left
+  constexpr bool AHEAD = NOP == 1;
+  __shared__ __attribute__((aligned(16))) char lds[(NOP + 2 + AHEAD) * OP];
   __shared__ __attribute__((aligned(16))) float sd[128], sp[128];
   char* const op = lds;             // O, then P: planes hi, lo
   char* const xb = lds + NOP * OP;  // a slab of X: planes hi, lo
+  char* const nx = AHEAD ? xb + 2 * OP : xb;  // a slab of the new X
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wid >> 2, wn = wid & 3;  // waves of 64 x 32
@@ -584,12 +635,12 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
   const uint32_t vt = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ (((lane >> 5) & 1) << 1)) << 4));
   const int cr = (q4 ^ key(r16 >> 2)) << 4;
   const int rt = 8 * q4 + (r16 >> 2), ct0 = (r16 & 3) >> 1, ct1 = (r16 & 1) * 8;
-  // byte of (row, column 32 cb + 16 h + 4 q4) in a plane, with either order of chunks
-  auto at_rows = [&](int row, int cb, int h) {
-    return cb * kBlkBytes + row * 64 + (((h * 2 + (q4 >> 1)) ^ key(row >> 2)) << 4) + (q4 & 1) * 8;
+  // byte of (row, column 32 cb + 8 q4) in a plane, with either order of chunks
+  auto at_rows = [&](int row, int cb) {
+    return cb * kBlkBytes + row * 64 + ((q4 ^ key(row >> 2)) << 4);
   };
-  auto at_cols = [&](int row, int cb, int h) {
-    return cb * kBlkBytes + row * 64 + (((h * 2 + (q4 >> 1)) ^ (((row >> 3) & 1) << 1)) << 4) + (q4 & 1) * 8;
+  auto at_cols = [&](int row, int cb) {
+    return cb * kBlkBytes + row * 64 + ((q4 ^ (((row >> 3) & 1) << 1)) << 4);
   };
   auto load_slab = [&](const Mat& x, int slab, uint32_t v, int planes) {
     for (int o = 0; o < planes; ++o) {
@@ -597,7 +648,7 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         const int q = wid * 4 + p;
-        load_lds<false>(d, xb + o * OP + q * 1024, v + (uint32_t)q * 1024u, 0);
+        load_lds<true>(d, xb + o * OP + q * 1024, v + (uint32_t)q * 1024u, 0);
       }
     }
   };
@@ -644,14 +695,19 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
   };
-  // hi (and lo) of x at (row, 4 columns) to a pair of planes at `base`
-  auto put = [&](char* base, int where, floatx4 x, bool lo) {
-    const f16x4 h = hi_of(x);
-    *(f16x4*)(base + where) = h;
-    if (lo) *(f16x4*)(base + OP + where) = lo_of(x, h);
+  // hi (and lo) of x at (row, 8 columns) to a pair of planes at `base`
+  auto put = [&](char* base, int where, const floatx4 (&x)[2], bool lo) {
+    const f16x4 h0 = hi_of(x[0]), h1 = hi_of(x[1]);
+    *(f16x8*)(base + where) = both(h0, h1);
+    if (lo) *(f16x8*)(base + OP + where) = both(lo_of(x[0], h0), lo_of(x[1], h1));
   };
   auto part_at = [&](int parity, int group) {
     return g.part + (((int64_t)bt * 2 + parity) * g.groups + group) * 16384 + (wid * 8 * 64 + lane) * 4;
+  };
+  // the waves meet with their LDS accesses done, but not their loads and stores of memory
+  auto meet = [] {
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    barrier_lds();
   };
   const std::false_type rows{};
   const std::true_type cols{};
@@ -665,7 +721,7 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
       wait_vm<0>();
       __syncthreads();
       products(gram, xb, xb, rows);
-      __syncthreads();  // the slab is read
+      meet();  // the slab is read
     }
     have = g.groups == 1;
   }
@@ -674,59 +730,72 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
     const Mat& Y = g.X[(it + 1) & 1];
     const bool last = it + 1 == g.steps;
     if (!have) {
+      // four parts on their way at a time: one after the other they took half of the step
       clear(gram);
-      for (int p = 0; p < g.groups; ++p) {
-        const float* const src = part_at(it & 1, p);
+      for (int p0 = 0; p0 < g.groups; p0 += 4) {
+        floatx4 v[4][8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int u = 0; u < 4; ++u) {
+          const float* const src = part_at(it & 1, min(p0 + u, g.groups - 1));
 #pragma unroll
-          for (int j = 0; j < 2; ++j) gram[i][j] += *(const floatx4*)(src + (i * 2 + j) * 256);
+          for (int x = 0; x < 8; ++x) v[u][x] = *(const floatx4*)(src + x * 256);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            if (p0 + u < g.groups) gram[x / 2][x % 2] += v[u][x];
+        }
       }
     }
     load_slab(X, s0, vt, 2);  // arrives behind the polynomial
-    // A = D + O
+    // A = D + O; from here on a lane's columns are 32 wn + 8 q4 + 4 j ..
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      widen(gram[i][0], gram[i][1]);
+      const int row = wm * 64 + i * 16 + r16;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int row = wm * 64 + i * 16 + r16, col = wn * 32 + j * 16 + q4 * 4;
-        floatx4 x = gram[i][j] * kInv;
+      for (int j = 0; j < 2; ++j) gram[i][j] *= kInv;
+      if (wm * 2 + i / 2 == wn) {  // meets the diagonal
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (row == col + q) {
-            sd[row] = x[q] * kInv;
-            x[q] = 0.f;
-          }
-        gram[i][j] = x;
-        put(op, at_rows(row, wn, j), x, NOP == 2);
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (row == wn * 32 + q4 * 8 + j * 4 + q) {
+              sd[row] = gram[i][j][q] * kInv;
+              gram[i][j][q] = 0.f;
+            }
       }
-    __builtin_amdgcn_s_waitcnt(0xC07F);
-    barrier_lds();  // not __syncthreads: the slab may still be on its way
+      put(op, at_rows(row, wn), gram[i], NOP == 2);
+    }
+    meet();
     floatx4 acc[4][2];
     clear(acc);
     products(acc, op, op, rows);
-    __builtin_amdgcn_s_waitcnt(0xC07F);
-    barrier_lds();  // O is read
+    meet();  // O is read
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      widen(acc[i][0], acc[i][1]);
       const int row = wm * 64 + i * 16 + r16;
       const float dr = sd[row];
+      floatx4 y[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int col = wn * 32 + j * 16 + q4 * 4;
+        const int col = wn * 32 + q4 * 8 + j * 4;
         const floatx4 dc = *(const floatx4*)(sd + col), s = gram[i][j];
-        floatx4 x = acc[i][j] * kInv;
+        const floatx4 x = acc[i][j] * kInv;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          if (row == col + q) {
-            sp[row] = g.a + g.b * dr + g.c * (x[q] * kInv + dr * dr);
-            x[q] = 0.f;
-          } else {
-            x[q] = g.b * s[q] + g.c * (x[q] + (dr + dc[q]) * s[q]);
-          }
+        for (int q = 0; q < 4; ++q) y[j][q] = g.b * s[q] + g.c * (x[q] + (dr + dc[q]) * s[q]);
+        if (wm * 2 + i / 2 == wn) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (row == col + q) {
+              sp[row] = g.a + g.b * dr + g.c * (x[q] * kInv + dr * dr);
+              y[j][q] = 0.f;
+            }
         }
-        put(op, at_rows(row, wn, j), x, NOP == 2);
       }
+      put(op, at_rows(row, wn), y, NOP == 2);
     }
     clear(gram);
     for (int s = s0; s < s1; ++s) {
@@ -736,64 +805,81 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
       products(acc, op, xb, cols);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
+        widen(acc[i][0], acc[i][1]);
         const int row = wm * 64 + i * 16 + r16;
         const float pr = sp[row];
+        const char* const x = xb + at_cols(row, wn);
+        const f16x8 h = *(const f16x8*)x, l = *(const f16x8*)(x + OP);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const char* const x = xb + at_cols(row, wn, j);
-          const floatx4 st = join((const _Float16*)x) + join((const _Float16*)(x + OP));
-          acc[i][j] = acc[i][j] * kInv + pr * st;
-        }
+        for (int j = 0; j < 2; ++j) acc[i][j] = acc[i][j] * kInv + pr * (wide(h, j) + wide(l, j));
       }
-      __syncthreads();  // the slab is read
+      meet();  // the slab is read
+      if (AHEAD && s + 1 < s1 && !last) load_slab(X, s + 1, vt, 2);
       if (!last) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int row = wm * 64 + i * 16 + r16, col = s * 128 + wn * 32 + j * 16 + q4 * 4;
-            const int64_t o = bt * Y.step + blk_at(row, col, g.np);
-            const f16x4 h = hi_of(acc[i][j]), l = lo_of(acc[i][j], h);
-            *(f16x4*)(Y.hi + o) = h;
-            *(f16x4*)(Y.lo + o) = l;
-            char* const x = xb + at_rows(row, wn, j);
-            *(f16x4*)x = h;
-            if (NOP == 2) *(f16x4*)(x + OP) = l;
-          }
-        __syncthreads();
-        products(gram, xb, xb, rows);
+        for (int i = 0; i < 4; ++i) {
+          const int row = wm * 64 + i * 16 + r16;
+          const int64_t o = bt * Y.step + blk_at(row, s * 128 + wn * 32 + q4 * 8, g.np);
+          const f16x4 h0 = hi_of(acc[i][0]), h1 = hi_of(acc[i][1]);
+          const f16x8 h = both(h0, h1), l = both(lo_of(acc[i][0], h0), lo_of(acc[i][1], h1));
+          *(f16x8*)(Y.hi + o) = h;
+          *(f16x8*)(Y.lo + o) = l;
+          char* const x = nx + at_rows(row, wn);
+          *(f16x8*)x = h;
+          if (NOP == 2) *(f16x8*)(x + OP) = l;
+        }
+        meet();
+        products(gram, nx, nx, rows);
       } else if (!g.r.clip || g.r.clip->finite) {
         const Result& r = g.r;
         const int64_t M = r.flip ? r.cols : r.rows, N = r.flip ? r.rows : r.cols;
         const int64_t end = FLIP ? M : N;
         const float f = kInv * r.scale;
         float* const t = (float*)(xb + wid * 2048);  // of this wave
+        // element of the tile (i, j), and v, its place in its row of the result
+        auto place = [&](int i, int j, int64_t& v) {
+          const int r0 = wm * 64 + i * 16, c0 = s * 128 + wn * 32 + j * 16;
+          int64_t u = r0 + r16;
+          v = c0 + q4 * 4;
+          if (FLIP) {
+            u = c0 + r16;
+            v = r0 + q4 * 4;
+          }
+          if (u >= (FLIP ? N : M)) v = end;
+          return bt * r.batch_stride + u * r.row_stride + v;
+        };
+#pragma unroll
+        for (int i = 0; i < 4; ++i) narrow(acc[i][0], acc[i][1]);
+        floatx4 w[4][2];  // the weights, all on their way together
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            int64_t v;
+            const int64_t at = place(i, j, v);
+            w[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
+            if (r.weight && r.vec && v < end) w[i][j] = weights_at(r, at);
+          }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             floatx4 y = acc[i][j] * f;
-            const int r0 = wm * 64 + i * 16, c0 = s * 128 + wn * 32 + j * 16;
-            int64_t u = r0 + r16, v = c0 + q4 * 4;
             if (FLIP) {
               __builtin_amdgcn_wave_barrier();
               *(floatx4*)(t + r16 * 20 + q4 * 4) = y;
               __builtin_amdgcn_wave_barrier();
 #pragma unroll
               for (int q = 0; q < 4; ++q) y[q] = t[(q4 * 4 + q) * 20 + r16];
-              u = c0 + r16;
-              v = r0 + q4 * 4;
             }
-            if (u >= (FLIP ? N : M)) v = end;
-            const int64_t at = bt * r.batch_stride + u * r.row_stride + v;
-            floatx4 w = {0.f, 0.f, 0.f, 0.f};
-            if (r.weight && r.vec && v < end) w = weights_at(r, at);
-            result_at(r, at, v, end, y, w);
+            int64_t v;
+            const int64_t at = place(i, j, v);
+            result_at(r, at, v, end, y, w[i][j]);
           }
       }
-      if (s + 1 < s1) {
-        __syncthreads();  // the new slab is read
-        load_slab(X, s + 1, vt, 2);
+      if (!AHEAD || last) {
+        meet();  // the new slab, or the transposed tiles, are read
+        if (s + 1 < s1) load_slab(X, s + 1, vt, 2);
       }
     }
     have = g.groups == 1;
