@@ -225,6 +225,7 @@ __device__ __forceinline__ void wait_vm() {
 // out while the other multiplies) of 64 x 32 (TP = 1) or 64 x 128 (TP = 2), KB blocks of 32
 // columns per stage, NS stages in LDS of which NS - 1 are on their way.
 constexpr int NT = 512;
+constexpr int kStrip = 8;
 template <int PROD, int EPI, bool FLIP, int TP, int NS>
 __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   constexpr int NOP = PROD == 3 ? 2 : 1;  // planes per operand
@@ -241,19 +242,37 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wid / WC, wn = wid % WC;  // 2 TP x WC waves
   const int r16 = lane & 15, q4 = lane >> 4;
-  const int bt = blockIdx.y;
-  int ti, tj;
+  // Workgroups go round the eight XCDs, each with an L2 of its own: XCD x takes the x-th eighth
+  // of all tiles, matrix by matrix and in each by strips of kStrip rows of tiles, so that what
+  // runs on one XCD at a time shares its panels.
+  int bt, ti, tj;
   {
-    const int t = blockIdx.x;
-    if (g.sym) {
-      // column by column of the upper triangle: tj (tj + 1) / 2 <= t
-      tj = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-      while (tj * (tj + 1) / 2 > t) --tj;
-      while ((tj + 1) * (tj + 2) / 2 <= t) ++tj;
-      ti = t - tj * (tj + 1) / 2;
-    } else {
-      ti = t % g.tm;
-      tj = t / g.tm;
+    const uint32_t w = blockIdx.y * gridDim.x + blockIdx.x, all = gridDim.x * gridDim.y;
+    const uint32_t x = w % 8, item = x * (all / 8) + min(x, all % 8) + w / 8;
+    bt = (int)(item / gridDim.x);
+    int t = (int)(item % gridDim.x), s = 0;
+    for (;; s += kStrip) {  // the strip from row s on
+      const int h = min(kStrip, g.tm - s);
+      const int n = g.sym ? h * (g.tn - s) - h * (h - 1) / 2 : h * g.tn;
+      if (t < n) {
+        if (!g.sym) {
+          ti = s + t % h;
+          tj = t / h;
+        } else {  // columns s .. s + h - 1 have 1 .. h tiles, the others h
+          const int tri = h * (h + 1) / 2;
+          if (t >= tri) {
+            ti = s + (t - tri) % h;
+            tj = s + h + (t - tri) / h;
+          } else {
+            int c = 0;
+            while (t > c) t -= ++c;
+            ti = s + t;
+            tj = s + c;
+          }
+        }
+        break;
+      }
+      t -= n;
     }
   }
   // Descriptors: the tile's panels that exist (everything past them reads as 0); in TR that of
@@ -1139,15 +1158,19 @@ Ws carve(void* base, const Plan& q) {
   return w;
 }
 
-// Tile side in panels for C of pm x pn panels (sym: its upper triangle).  A round of 256
-// tiles of 256 x 256 takes as long as four of 128 x 128 or longer, as far as both are
-// bound by the matrix instructions.
+// Tile side in panels for C of pm x pn panels (sym: its upper triangle), by rounds of 256
+// tiles.  Tiles of 256 x 256 need half the loads and LDS reads per product, tiles of
+// 128 x 128 fill the last round better and overlap their epilogues, two to a CU.  Where the
+// rounds are equally full the smaller tiles take 1.2 times as long with one product and 1.7
+// times with three, which read twice as much (whole updates, 256 against 128: 8192 x 8192
+// bf16 10.4 and 11.2 ms, 32 matrices of 768 x 1536 bf16 1.09 and 0.99 ms, 4096 x 4096 fp32
+// 3.86 and 4.41 ms, 5120 x 4096 bf16 2.28 and 2.11 ms).
 int tile_of(const Plan& q, int64_t pm, int64_t pn, bool sym) {
-  auto tiles = [&](int64_t t) {
+  auto rounds = [&](int64_t t) {
     const int64_t m = (pm + t - 1) / t, n = (pn + t - 1) / t;
-    return (sym ? m * (m + 1) / 2 : m * n) * q.batch;
+    return ((sym ? m * (m + 1) / 2 : m * n) * q.batch + 255) / 256;
   };
-  return tiles(2) >= 512 ? 2 : 1;
+  return rounds(1) * (q.three ? 42 : 30) > rounds(2) * 100 ? 2 : 1;
 }
 
 template <int EPI, bool FLIP = false>
