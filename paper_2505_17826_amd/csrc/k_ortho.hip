@@ -222,35 +222,44 @@ __device__ __forceinline__ void wait_vm() {
 }
 
 // Tiles of 128 TP x 128 TP, eight waves (two per SIMD: the loads and LDS reads of one go
-// out while the other multiplies) of 64 x 32 (TP = 1) or 64 x 128 (TP = 2), KB blocks of 32
-// columns per stage, NS stages in LDS of which NS - 1 are on their way.
+// out while the other multiplies) of 64 x 32 (TP = 1) or 64 x 128 (TP = 2), or tiles of
+// 64 x 128 and four waves of 64 x 32 (TP = 0); KB blocks of 32 columns per stage, NS stages
+// in LDS of which NS - 1 are on their way.
 constexpr int NT = 512;
 constexpr int kStrip = 8;
+constexpr int threads_of(int tp) { return tp ? NT : NT / 2; }
 template <int PROD, int EPI, bool FLIP, int TP, int NS>
-__global__ void __launch_bounds__(NT) k_ns(const Args g) {
+__global__ void __launch_bounds__(threads_of(TP), 2) k_ns(const Args g) {
   constexpr int NOP = PROD == 3 ? 2 : 1;  // planes per operand
   constexpr int KB = PROD == 3 ? 1 : 2;
   constexpr bool TR = EPI == APPLY || EPI == LAST;
-  constexpr int OPB = KB * TP * kBlkBytes;  // bytes of an operand plane in a stage
-  constexpr int STAGE = 2 * NOP * OPB;
-  constexpr int WC = TP == 1 ? 4 : 2;       // waves along the columns
-  constexpr int WN = 8 * TP / WC;           // 16-column tiles of a wave
-  constexpr int SETS = TP == 1 ? 2 : 1;     // of fragments in registers
-  constexpr int SB = TP == 1 ? 2 : 1;       // rows of tiles whose epilogue operands are held
+  constexpr int NW = threads_of(TP) / 64;
+  constexpr int CP = TP ? TP : 1;              // panels of B
+  constexpr int PA = TP ? 8 * TP : 4, PB = 8 * CP;  // 16-row pieces of an operand's block
+  constexpr int OPA = KB * PA * 1024, OPB = KB * PB * 1024;  // bytes of a plane in a stage
+  constexpr int STAGE = NOP * (OPA + OPB);
+  constexpr int WC = TP == 2 ? 2 : 4;       // waves along the columns
+  constexpr int WN = 8 * CP / WC;           // 16-column tiles of a wave
+  constexpr int SETS = TP == 2 ? 1 : 2;     // of fragments in registers
+  constexpr int SB = TP == 2 ? 1 : 2;       // rows of tiles whose epilogue operands are held
   __shared__ __attribute__((aligned(16))) char lds[NS * STAGE];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wid / WC, wn = wid % WC;  // 2 TP x WC waves
+  const int wm = wid / WC, wn = wid % WC;
   const int r16 = lane & 15, q4 = lane >> 4;
   // Workgroups go round the eight XCDs, each with an L2 of its own: XCD x takes the x-th eighth
   // of all tiles, matrix by matrix and in each by strips of kStrip rows of tiles, so that what
   // runs on one XCD at a time shares its panels.
-  int bt, ti, tj;
+  int bt, ti, tj, half = 0;
   {
     const uint32_t w = blockIdx.y * gridDim.x + blockIdx.x, all = gridDim.x * gridDim.y;
     const uint32_t x = w % 8, item = x * (all / 8) + min(x, all % 8) + w / 8;
     bt = (int)(item / gridDim.x);
     int t = (int)(item % gridDim.x), s = 0;
+    if (TP == 0) {
+      half = t & 1;  // of the 128 rows of a tile
+      t >>= 1;
+    }
     for (;; s += kStrip) {  // the strip from row s on
       const int h = min(kStrip, g.tm - s);
       const int n = g.sym ? h * (g.tn - s) - h * (h - 1) / 2 : h * g.tn;
@@ -278,13 +287,13 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   // Descriptors: the tile's panels that exist (everything past them reads as 0); in TR that of
   // B covers the 128 rows of X that a k-step lies in, and moves on with k.
   const int panel = g.K * 256;                       // bytes of a panel of A (and of B)
-  const int64_t oA = bt * g.A.step + (int64_t)ti * TP * (panel / 2);
-  const int nA = min(TP, g.pa - ti * TP) * panel;
+  const int64_t oA = bt * g.A.step + (int64_t)ti * CP * (panel / 2) + half * (kBlk / 2);
+  const int nA = min(CP, g.pa - ti * CP) * panel - half * (kBlkBytes / 2);
   const Desc rA = desc(g.A.hi + oA, nA);
   const Desc rAl = desc((NOP == 2 ? g.A.lo : g.A.hi) + oA, nA);
   const int rowsB = TR ? g.np * 256 : panel;         // bytes of 128 rows of B
-  const int64_t oB = bt * g.B.step + (TR ? 0 : (int64_t)tj * TP * (panel / 2));
-  const int nB = TR ? rowsB : min(TP, g.pb - tj * TP) * panel;
+  const int64_t oB = bt * g.B.step + (TR ? 0 : (int64_t)tj * CP * (panel / 2));
+  const int nB = TR ? rowsB : min(CP, g.pb - tj * CP) * panel;
   const Desc rB = desc(g.B.hi + oB, nB);
   const Desc rBl = desc((NOP == 2 ? g.B.lo : g.B.hi) + oB, nB);
   // LDS rows of 64 bytes.  Read along the rows (a 16-byte chunk of 16 rows by each of four
@@ -297,37 +306,38 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   auto key = [](int x) { return (0x78 >> (2 * (x & 3))) & 3; };
   const uint32_t vr = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ key(lane >> 4)) << 4));
   const uint32_t vt = (uint32_t)((lane >> 2) * 64 + (((lane & 3) ^ (((lane >> 5) & 1) << 1)) << 4));
-  constexpr int NI = KB * TP;  // instructions per wave, operand plane and stage
+  constexpr int NA = KB * PA / NW, NB = KB * PB / NW;  // load instructions per wave, plane and stage
   // What may pass a descriptor's end goes into the vector part of the offset, which is what
   // the hardware compares; a stage past the last reads zeros (off = 2^31), so that the loop
   // has no branches.
-  auto load_row = [&](const Desc& r, char* dst, int kt, uint32_t off, int p) {
-    const int q = wid * NI + p, kb = q / (8 * TP), pn = (q >> 3) % TP, part = q & 7;
+  auto load_row = [&](const Desc& r, char* dst, int kt, uint32_t off, int q, int pieces) {
+    const int kb = q / pieces, pn = pieces < 8 ? 0 : (q >> 3) % (pieces / 8), part = q & (min(pieces, 8) - 1);
     load_lds<TR>(r, dst + q * 1024,
                  vr + ((uint32_t)(pn * panel + kb * kBlkBytes + part * 1024) | off), kt * KB * kBlkBytes);
   };
-  // 32 rows (from 32 kt KB on) x 128 TP columns: 4 TP blocks' 2 KiB pieces
-  auto load_col = [&](const Desc& r, char* dst, int kt, uint32_t off, int p) {
-    const int q = wid * NI + p, kb = q / (8 * TP), cb = (q >> 1) % (4 * TP), half = q & 1;
+  // 32 rows (from 32 kt KB on) x 128 CP columns: 4 CP blocks' 2 KiB pieces
+  auto load_col = [&](const Desc& r, char* dst, int kt, uint32_t off, int q) {
+    const int kb = q / PB, cb = (q >> 1) % (4 * CP), part = q & 1;
     const int k0 = (kt * KB & 3) * 32;
     load_lds<TR>(r, dst + q * 1024,
-                 vt + ((uint32_t)((tj * 4 * TP + cb) * kBlkBytes + kb * 2048 + half * 1024) | off), k0 * 64);
+                 vt + ((uint32_t)((tj * 4 * CP + cb) * kBlkBytes + kb * 2048 + part * 1024) | off), k0 * 64);
   };
   const int nk = g.K / (BC * KB);  // K is a multiple of 128: nk is even where KB = 1
-  constexpr int L = 2 * NOP * NI;  // load instructions per wave and stage
-  // The x-th load of stage t: operand planes A, B, and of lo planes A, B, NI each.
+  constexpr int L = NOP * (NA + NB);  // load instructions per wave and stage
+  // The x-th load of stage t: of A and B, then of their lo planes.
   auto load_one = [&](char* dst, int t, int x) {
-    const int kt = t < nk ? t : 0, plane = x / NI, p = x % NI;
+    const int kt = t < nk ? t : 0;
     const uint32_t off = t < nk ? 0u : 0x80000000u;
-    const bool lo = plane >= 2;
-    char* const d = dst + plane * OPB;
-    if (plane % 2 == 0) {
-      load_row(lo ? rAl : rA, d, kt, off, p);
+    const bool lo = x >= NA + NB;
+    const int y = x % (NA + NB);
+    char* const d = dst + (lo ? OPA + OPB : 0);
+    if (y < NA) {
+      load_row(lo ? rAl : rA, d, kt, off, wid * NA + y, PA);
     } else if (TR) {
       const int64_t o = oB + (int64_t)(kt * KB >> 2) * (rowsB / 2);
-      load_col(desc((lo ? g.B.lo : g.B.hi) + o, rowsB), d, kt, off, p);
+      load_col(desc((lo ? g.B.lo : g.B.hi) + o, rowsB), d + OPA, kt, off, wid * NB + y - NA);
     } else {
-      load_row(lo ? rBl : rB, d, kt, off, p);
+      load_row(lo ? rBl : rB, d + OPA, kt, off, wid * NB + y - NA, PB);
     }
   };
   auto load = [&](char* dst, int t) {
@@ -351,8 +361,8 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
   s16x4 fh[SETS][NOP][WN][2];  // TR: halves of fb
   auto read_one = [&](int set, const char* st, int kb, int x) {
     const int o = x / (4 + BR), y = x % (4 + BR);
-    const char* sa = st + 2 * o * OPB + kb * (TP * kBlkBytes) + (wm * 64 + r16) * 64 + cr;
-    const char* sb = st + (2 * o + 1) * OPB + kb * (TP * kBlkBytes);
+    const char* sa = st + o * (OPA + OPB) + kb * (PA * 1024) + (wm * 64 + r16) * 64 + cr;
+    const char* sb = st + o * (OPA + OPB) + OPA + kb * (PB * 1024);
     if (y < 4) {
       fa[set][o][y] = *(const f16x8*)(sa + y * 1024);
     } else if (TR) {
@@ -387,6 +397,11 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
     // Few products per fragment: the fragments of the next 32 columns are read, and the next
     // stage's loads issued, between the products of this one.
     constexpr int UN = KB == 1 ? 2 : 1;  // stages per turn of the loop: the sets alternate
+    // One wave per SIMD (TP = 0): the reads go out before the first third of the products and
+    // have the others to arrive (three products at 1000 x 2223, Gram: 27.3 -> 25.6 us).  With
+    // two waves the even spread does as well and keeps fewer fragments in registers.
+    constexpr bool EARLY = TP == 0;
+    constexpr int QR = PD / 3;
 #pragma unroll
     for (int x = 0; x < RD; ++x) read_one(0, lds, 0, x);
     for (int kt = 0; kt < nk; kt += UN) {
@@ -401,12 +416,16 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
         }
         const char* const st = lds + cur * STAGE;
         const int extra = RD + (last ? L : 0);
+        auto at = [&](int q) {  // reads and loads issued before product q
+          if (!EARLY) return q * extra / PD;
+          return q < QR ? q * RD / QR : RD + (q - QR) * (extra - RD) / (PD - QR);
+        };
 #pragma unroll
         for (int q = 0; q < PD; ++q) {
           multiply_one(set, q);
           // past the last stage the reads are not used
 #pragma unroll
-          for (int x = q * extra / PD; x < (q + 1) * extra / PD; ++x) {
+          for (int x = at(q); x < at(q + 1); ++x) {
             if (x < RD)
               read_one(set ^ 1, st, (u + 1) % KB, x);
             else
@@ -437,7 +456,7 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
 
   // ------------------------------------------------------------------ epilogue
   // element q of tile (i, j): row i0 + 16 i + r16, column j0 + 16 j + 4 q4 + q
-  const int i0 = (ti * TP + (wm >> 1)) * 128 + (wm & 1) * 64, j0 = tj * TP * 128 + wn * 16 * WN;
+  const int i0 = ti * CP * 128 + (TP ? wm : half) * 64, j0 = tj * CP * 128 + wn * 16 * WN;
   char* const mine = lds + wid * 2048;  // of this wave: a tile or two at a time
   if (i0 >= g.mp) return;
   // What a row of tiles needs from memory is loaded whole, that of the next row before this
@@ -616,7 +635,7 @@ __global__ void __launch_bounds__(NT) k_ns(const Args g) {
 // ------------------------------------------------------- up to 128 rows --
 // Matrices whose shorter side is at most 128: A, its polynomial and the products with X fit
 // one workgroup, and what the three kernels above spend on such matrices is launches and
-// latencies (12, 6 and 8 us per step at 128 x 1536).  A workgroup owns `per` slabs of 128
+// latencies (12, 6 and 8 us per step at 128 x 1536; a step here takes 19).  A workgroup owns `per` slabs of 128
 // columns of X.  A step of a slab takes P X, the new X and its part of X X^T (64 KiB of X in
 // LDS); A and P are formed by every workgroup of a matrix for itself, from the parts of A
 // that the last launch left (the end of a launch is what orders the workgroups).  A matrix
@@ -1184,6 +1203,12 @@ hipError_t product(const Plan& q, Args& g, hipStream_t s) {
     constexpr int P = decltype(prod)::value;
     if (t == 2)
       k_ns<P, EPI, FLIP, 2, 2><<<grid, NT, 0, s>>>(g);
+    else if (tiles * q.batch <= 128)
+      // half the CUs or fewer would have work: tiles of 64 rows (Gram product of 1536 x 1536
+      // bf16, 78 tiles: 13.9 -> 11.4 us, of 1000 x 2223 fp32, 36 tiles: 35 -> 25.6 us; with
+      // 144 tiles they are slower, 18.4 -> 19.9 us).  Three stages fit two workgroups to a
+      // CU; four and six took 14 us, and the compiler moved the sums between register files.
+      k_ns<P, EPI, FLIP, 0, 3><<<dim3(2 * grid.x, grid.y), NT / 2, 0, s>>>(g);
     else if (tiles * q.batch <= 256)
       k_ns<P, EPI, FLIP, 1, 4><<<grid, NT, 0, s>>>(g);
     else
