@@ -635,11 +635,12 @@ __global__ void __launch_bounds__(threads_of(TP), 2) k_ns(const Args g) {
 // ------------------------------------------------------- up to 128 rows --
 // Matrices whose shorter side is at most 128: A, its polynomial and the products with X fit
 // one workgroup, and what the three kernels above spend on such matrices is launches and
-// latencies (12, 6 and 8 us per step at 128 x 1536; a step here takes 19).  A workgroup owns `per` slabs of 128
-// columns of X.  A step of a slab takes P X, the new X and its part of X X^T (64 KiB of X in
-// LDS); A and P are formed by every workgroup of a matrix for itself, from the parts of A
-// that the last launch left (the end of a launch is what orders the workgroups).  A matrix
-// with one workgroup runs all its steps in one launch.
+// latencies (12, 6 and 8 us per step at 128 x 1536; a step here takes 19, of which 5.4 are
+// the reading of six workgroups' parts of A and 4.1 each of two slabs).  A workgroup owns
+// `per` slabs of 128 columns of X.  A step of a slab takes P X, the new X and its part of
+// X X^T (64 KiB of X in LDS); A and P are formed by every workgroup of a matrix for itself,
+// from the parts of A that the last launch left (the end of a launch is what orders the
+// workgroups).  A matrix with one workgroup runs all its steps in one launch.
 struct SmallArgs {
   Mat X[2];      // ping-pong
   float* part;   // [batch][2][groups][128 x 128] parts of A, by lane
