@@ -39,6 +39,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr int kPad = 128;  // rows and columns are padded to it
@@ -64,6 +65,7 @@ struct Mat {
 struct Result {  // of LAST
   int flip;      // X is the transpose of the caller's matrix
   int vec;       // four elements of a row at a time (alignment, strides)
+  int vec8;      // eight, of a bf16 result without a master
   int64_t rows, cols, row_stride, batch_stride;
   void* out;     // rft_orthogonalize: out = scale X
   int out_bf16;
@@ -104,6 +106,21 @@ __device__ __forceinline__ void barrier_lds() {
   asm volatile("" ::: "memory");
 }
 
+// Contractions are written out: which of two products of a sum is fused must not differ from
+// one variant of a kernel to another, which give a matrix the same bits.
+__device__ __forceinline__ floatx4 fma4(floatx4 a, floatx4 b, floatx4 c) {
+  return __builtin_elementwise_fma(a, b, c);
+}
+__device__ __forceinline__ floatx4 fma4(float a, floatx4 b, floatx4 c) {
+  return __builtin_elementwise_fma((floatx4){a, a, a, a}, b, c);
+}
+// P off and on the diagonal, from an element x of O O.
+__device__ __forceinline__ float poly_off(float b, float c, float di, float dj, float o, float x) {
+  return fmaf(c, fmaf(di + dj, o, x), b * o);
+}
+__device__ __forceinline__ float poly_diag(float a, float b, float c, float d, float x) {
+  return fmaf(c, fmaf(d, d, x), fmaf(b, d, a));
+}
 __device__ __forceinline__ f16x4 hi_of(floatx4 x) { return __builtin_convertvector(x, f16x4); }
 __device__ __forceinline__ f16x4 lo_of(floatx4 x, f16x4 h) {
   return __builtin_convertvector(x - __builtin_convertvector(h, floatx4), f16x4);
@@ -155,6 +172,19 @@ __device__ __forceinline__ floatx4 weights_at(const Result& r, int64_t at) {
   const u16x4 h = *(const u16x4*)((const uint16_t*)r.weight + at);
   return (floatx4){bf16_to_f32(h[0]), bf16_to_f32(h[1]), bf16_to_f32(h[2]), bf16_to_f32(h[3])};
 }
+// Eight bf16 elements at `at` (r.vec8): the weights there, and the result from y0, y1.
+__device__ __forceinline__ u16x8 weights8_at(const Result& r, int64_t at) {
+  return *(const u16x8*)((const uint16_t*)r.weight + at);
+}
+__device__ __forceinline__ void result8_at(const Result& r, int64_t at, floatx4 y0, floatx4 y1, u16x8 w) {
+  u16x8 z;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const float y = q < 4 ? y0[q & 3] : y1[q & 3];
+    z[q] = f32_to_bf16(r.weight ? fmaf(bf16_to_f32(w[q]), r.decay, -y) : y);
+  }
+  *(u16x8*)((uint16_t*)(r.weight ? r.weight : r.out) + at) = z;
+}
 // The result y (scaled) of elements [v, v + 4) of a row that ends at `end`, at `at`; w: the
 // weights there (r.vec, which implies that the row's length is a multiple of four).
 __device__ __forceinline__ void result_at(const Result& r, int64_t at, int64_t v, int64_t end,
@@ -164,7 +194,7 @@ __device__ __forceinline__ void result_at(const Result& r, int64_t at, int64_t v
   const bool half = r.weight ? r.weight_bf16 : r.out_bf16;
   if (r.vec) {
     if (r.weight) {
-      y = w * r.decay - y;
+      y = fma4(r.decay, w, -y);
       if (r.master) *(floatx4*)(r.master + at) = y;
     }
     if (half)
@@ -182,7 +212,7 @@ __device__ __forceinline__ void result_at(const Result& r, int64_t at, int64_t v
       const float w0 = r.master ? r.master[at + q]
                        : r.weight_bf16 ? bf16_to_f32(((const uint16_t*)r.weight)[at + q])
                                        : ((const float*)r.weight)[at + q];
-      z = w0 * r.decay - z;
+      z = fmaf(w0, r.decay, -z);
       if (r.master) r.master[at + q] = z;
     }
     if (half)
@@ -496,6 +526,32 @@ __global__ void __launch_bounds__(threads_of(TP), 2) k_ns(const Args g) {
       if (r.weight && r.vec && j0 + j * 16 < g.np && v < end) w[j] = weights_at(r, at);
     };
     if (SB == 2) state(0, 0);
+    if (!FLIP && r.vec8) {
+      // eight columns per lane where a bf16 result allows it (32 matrices of 768 x 1536: 156
+      // -> 132 us); of an fp32 result four columns per lane fill 64 bytes of a row
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t u = i0 + i * 16 + r16, v0 = j0 + q4 * 8;
+        const int64_t at = bt * r.batch_stride + u * r.row_stride + v0;
+        if (SB == 1) state(i, 0);
+        u16x8 w8[WP];
+#pragma unroll
+        for (int j = 0; j < WP; ++j)
+          if (r.weight && u < M && v0 + j * 32 < N) w8[j] = weights8_at(r, at + j * 32);
+        if (SB == 2 && i + 1 < 4) state(i + 1, (i + 1) & 1);
+#pragma unroll
+        for (int j = 0; j < WP; ++j) {
+          if (j0 + j * 32 >= g.np) continue;
+          widen(acc[i][2 * j], acc[i][2 * j + 1]);
+          const floatx4 x0 = wide(sh[i % SB][j], 0) + wide(sl[i % SB][j], 0);
+          const floatx4 x1 = wide(sh[i % SB][j], 1) + wide(sl[i % SB][j], 1);
+          if (u < M && v0 + j * 32 < N)
+            result8_at(r, at + j * 32, fma4(pi[i % SB], x0, acc[i][2 * j] * kInv) * f,
+                       fma4(pi[i % SB], x1, acc[i][2 * j + 1] * kInv) * f, w8[j]);
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (SB == 1) state(i, 0);
@@ -504,28 +560,28 @@ __global__ void __launch_bounds__(threads_of(TP), 2) k_ns(const Args g) {
         for (int j = 0; j < WN; ++j) old(i, j);
       }
       if (SB == 2 && i + 1 < 4) state(i + 1, (i + 1) & 1);
-      floatx4 x[2];
 #pragma unroll
-      for (int j = 0; j < WN; ++j) {
-        if (j0 + j * 16 >= g.np) continue;
-        if (j % 2 == 0) {
-          x[0] = wide(sh[i % SB][j / 2], 0) + wide(sl[i % SB][j / 2], 0);
-          x[1] = wide(sh[i % SB][j / 2], 1) + wide(sl[i % SB][j / 2], 1);
-          narrow(x[0], x[1]);
-        }
-        floatx4 y = (pi[i % SB] * x[j % 2] + acc[i][j] * kInv) * f;
-        if (FLIP) {  // the tile transposed through LDS, rows 20 floats apart
-          float* const t = (float*)mine;
-          __builtin_amdgcn_wave_barrier();
-          *(floatx4*)(t + r16 * 20 + q4 * 4) = y;
-          __builtin_amdgcn_wave_barrier();
+      for (int j = 0; j < WP; ++j) {
+        if (j0 + j * 32 >= g.np) continue;
+        floatx4 x0 = wide(sh[i % SB][j], 0) + wide(sl[i % SB][j], 0);
+        floatx4 x1 = wide(sh[i % SB][j], 1) + wide(sl[i % SB][j], 1);
+        if (SB == 1) old(i, 2 * j), old(i, 2 * j + 1);
+        narrow(x0, x1);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) y[q] = t[(q4 * 4 + q) * 20 + r16];
+        for (int e = 0; e < 2; ++e) {
+          floatx4 y = fma4(pi[i % SB], e ? x1 : x0, acc[i][2 * j + e] * kInv) * f;
+          if (FLIP) {  // the tile transposed through LDS, rows 20 floats apart
+            float* const t = (float*)mine;
+            __builtin_amdgcn_wave_barrier();
+            *(floatx4*)(t + r16 * 20 + q4 * 4) = y;
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = t[(q4 * 4 + q) * 20 + r16];
+          }
+          int64_t v;
+          const int64_t at = place(i, 2 * j + e, v);
+          result_at(r, at, v, end, y, w[2 * j + e]);
         }
-        int64_t v;
-        const int64_t at = place(i, j, v);
-        if (SB == 1) old(i, j);
-        result_at(r, at, v, end, y, w[j]);
       }
     }
   } else {
@@ -534,7 +590,10 @@ __global__ void __launch_bounds__(threads_of(TP), 2) k_ns(const Args g) {
     constexpr bool HI = EPI != GRAM, LO = EPI == APPLY || (EPI == POLY && NOP == 2);
     const int kp = EPI == APPLY ? g.np : g.mp;
     const int64_t vb = (int64_t)bt * g.mp;
-    const bool mirror = EPI != APPLY && ti != tj;
+    // of the panels beside the diagonal in one tile (TP = 2), those above it are stored both
+    // ways round too: below it the products hi lo and lo hi come in the other order
+    const bool mirror = EPI != APPLY && (i0 >> 7) < (j0 >> 7);
+    if (EPI != APPLY && (i0 >> 7) > (j0 >> 7)) return;
     constexpr int WP = WN / 2;  // pairs of tiles: a lane's columns are j0 + 32 j + 8 q4 ..
     f16x8 sh[SB][WP], sl[SB][WP];
     float di[SB] = {};
@@ -592,18 +651,18 @@ __global__ void __launch_bounds__(threads_of(TP), 2) k_ns(const Args g) {
             if (SB == 1) dj[j][e] = *(const floatx4*)(g.d + vb + col);
             floatx4 y;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) y[q] = g.b * s[q] + g.c * (x[q] + (dr + dj[j][e][q]) * s[q]);
+            for (int q = 0; q < 4; ++q) y[q] = poly_off(g.b, g.c, dr, dj[j][e][q], s[q], x[q]);
             if (on) {
 #pragma unroll
               for (int q = 0; q < 4; ++q)
                 if (row == col + q) {
-                  g.p[vb + row] = g.a + g.b * dr + g.c * (x[q] * kInv + dr * dr);
+                  g.p[vb + row] = poly_diag(g.a, g.b, g.c, dr, x[q] * kInv);
                   y[q] = 0.f;
                 }
             }
             x = y;
           } else {
-            x += di[i % SB] * s;
+            x = fma4(di[i % SB], s, x);
           }
           h[e] = hi_of(x);
           // lo planes: of X always, of the others where products use them
@@ -824,12 +883,12 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
         const floatx4 dc = *(const floatx4*)(sd + col), s = gram[i][j];
         const floatx4 x = acc[i][j] * kInv;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) y[j][q] = g.b * s[q] + g.c * (x[q] + (dr + dc[q]) * s[q]);
+        for (int q = 0; q < 4; ++q) y[j][q] = poly_off(g.b, g.c, dr, dc[q], s[q], x[q]);
         if (wm * 2 + i / 2 == wn) {
 #pragma unroll
           for (int q = 0; q < 4; ++q)
             if (row == col + q) {
-              sp[row] = g.a + g.b * dr + g.c * (x[q] * kInv + dr * dr);
+              sp[row] = poly_diag(g.a, g.b, g.c, dr, x[q] * kInv);
               y[j][q] = 0.f;
             }
         }
@@ -850,7 +909,7 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
         const char* const x = xb + at_cols(row, wn);
         const f16x8 h = *(const f16x8*)x, l = *(const f16x8*)(x + OP);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = acc[i][j] * kInv + pr * (wide(h, j) + wide(l, j));
+        for (int j = 0; j < 2; ++j) acc[i][j] = fma4(pr, wide(h, j) + wide(l, j), acc[i][j] * kInv);
       }
       meet();  // the slab is read
       if (AHEAD && s + 1 < s1 && !last) load_slab(X, s + 1, vt, 2);
@@ -875,46 +934,63 @@ __global__ void __launch_bounds__(NT) k_ns_small(const SmallArgs g) {
         const int64_t end = FLIP ? M : N;
         const float f = kInv * r.scale;
         float* const t = (float*)(xb + wid * 2048);  // of this wave
-        // element of the tile (i, j), and v, its place in its row of the result
-        auto place = [&](int i, int j, int64_t& v) {
-          const int r0 = wm * 64 + i * 16, c0 = s * 128 + wn * 32 + j * 16;
-          int64_t u = r0 + r16;
-          v = c0 + q4 * 4;
-          if (FLIP) {
-            u = c0 + r16;
-            v = r0 + q4 * 4;
-          }
-          if (u >= (FLIP ? N : M)) v = end;
-          return bt * r.batch_stride + u * r.row_stride + v;
-        };
+        if (!FLIP && r.vec8) {  // as in k_ns
+          u16x8 w8[4];
+          bool in[4];
+          int64_t at[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) narrow(acc[i][0], acc[i][1]);
-        floatx4 w[4][2];  // the weights, all on their way together
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            int64_t v;
-            const int64_t at = place(i, j, v);
-            w[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
-            if (r.weight && r.vec && v < end) w[i][j] = weights_at(r, at);
+          for (int i = 0; i < 4; ++i) {
+            const int64_t u = wm * 64 + i * 16 + r16, v = s * 128 + wn * 32 + q4 * 8;
+            in[i] = u < M && v < N;
+            at[i] = bt * r.batch_stride + u * r.row_stride + v;
+            w8[i] = (u16x8){0, 0, 0, 0, 0, 0, 0, 0};
+            if (r.weight && in[i]) w8[i] = weights8_at(r, at[i]);
           }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            floatx4 y = acc[i][j] * f;
+          for (int i = 0; i < 4; ++i)
+            if (in[i]) result8_at(r, at[i], acc[i][0] * f, acc[i][1] * f, w8[i]);
+        } else {
+          // element of the tile (i, j), and v, its place in its row of the result
+          auto place = [&](int i, int j, int64_t& v) {
+            const int r0 = wm * 64 + i * 16, c0 = s * 128 + wn * 32 + j * 16;
+            int64_t u = r0 + r16;
+            v = c0 + q4 * 4;
             if (FLIP) {
-              __builtin_amdgcn_wave_barrier();
-              *(floatx4*)(t + r16 * 20 + q4 * 4) = y;
-              __builtin_amdgcn_wave_barrier();
-#pragma unroll
-              for (int q = 0; q < 4; ++q) y[q] = t[(q4 * 4 + q) * 20 + r16];
+              u = c0 + r16;
+              v = r0 + q4 * 4;
             }
-            int64_t v;
-            const int64_t at = place(i, j, v);
-            result_at(r, at, v, end, y, w[i][j]);
-          }
+            if (u >= (FLIP ? N : M)) v = end;
+            return bt * r.batch_stride + u * r.row_stride + v;
+          };
+#pragma unroll
+          for (int i = 0; i < 4; ++i) narrow(acc[i][0], acc[i][1]);
+          floatx4 w[4][2];  // the weights, all on their way together
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              int64_t v;
+              const int64_t at = place(i, j, v);
+              w[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
+              if (r.weight && r.vec && v < end) w[i][j] = weights_at(r, at);
+            }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              floatx4 y = acc[i][j] * f;
+              if (FLIP) {
+                __builtin_amdgcn_wave_barrier();
+                *(floatx4*)(t + r16 * 20 + q4 * 4) = y;
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) y[q] = t[(q4 * 4 + q) * 20 + r16];
+              }
+              int64_t v;
+              const int64_t at = place(i, j, v);
+              result_at(r, at, v, end, y, w[i][j]);
+            }
+        }
       }
       if (!AHEAD || last) {
         meet();  // the new slab, or the transposed tiles, are read
@@ -1310,6 +1386,11 @@ bool by_four(const rft_matrices& x, const void* p, int bytes) {
   return !p || (x.cols % 4 == 0 && (x.rows == 1 || x.row_stride % 4 == 0) &&
                 (x.batch <= 1 || x.batch_stride % 4 == 0) && (uintptr_t)p % (4 * bytes) == 0);
 }
+// The same for eight elements of bf16 arrays.
+bool by_eight(const rft_matrices& x, const void* p) {
+  return x.cols % 8 == 0 && (x.rows == 1 || x.row_stride % 8 == 0) &&
+         (x.batch <= 1 || x.batch_stride % 8 == 0) && (uintptr_t)p % 16 == 0;
+}
 int bytes_of(int dtype) { return dtype == RFT_BF16 ? 2 : 4; }
 
 // Finite also as a float.
@@ -1384,6 +1465,7 @@ rft_status rft_orthogonalize(const rft_matrices* mats, const void* g, int dtype,
   r.out = out;
   r.vec = by_four(*mats, out, bytes_of(out_dtype));
   r.out_bf16 = out_dtype == RFT_BF16;
+  r.vec8 = r.out_bf16 && by_eight(*mats, out);
   r.scale = (float)params->scale;
   RFT_HIP(ns::orthogonalize(q, in, r, *params, w, (hipStream_t)stream), fn);
   return RFT_OK;
@@ -1425,6 +1507,7 @@ rft_status rft_muon_step(const rft_matrices* mats, const void* grad, int grad_dt
   r.vec = by_four(*mats, weight, bytes_of(weight_dtype)) && by_four(*mats, master, 4);
   r.weight_bf16 = weight_dtype == RFT_BF16;
   r.master = master;
+  r.vec8 = r.weight_bf16 && !master && by_eight(*mats, weight);
   r.decay = (float)(1.0 - params->lr * params->weight_decay);
   r.scale = (float)(params->lr * params->scale);
   r.clip = clip;

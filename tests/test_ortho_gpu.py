@@ -99,6 +99,44 @@ def test_stacks_and_strides(shape):
     assert torch.equal(o, whole) and torch.equal(torch.isnan(buf), gaps)
 
 
+@pytest.mark.parametrize("shape", [(40, 512, 768), (48, 1000, 1100)])
+@pytest.mark.parametrize("products", [R.RFT_PRODUCTS_ONE, R.RFT_PRODUCTS_THREE])
+def test_tile_sizes_give_the_same_bits(shape, products):
+    """A large stack takes larger tiles than its matrices alone, the larger one also in its
+    symmetric products."""
+    x = matrix(9, *shape).to(DEV)
+    p = R.muon_params(products=products)
+    whole = R.rft_orthogonalize(x, p)
+    for i in (0, 23, 39):
+        assert torch.equal(R.rft_orthogonalize(x[i], p), whole[i])
+
+
+@pytest.mark.parametrize("shape", [(2, 130, 264), (1, 100, 1000), (2, 300, 136), (3, 128, 8), (40, 512, 768)])
+def test_alignment_of_bf16_results(shape):
+    """Results stored eight, four and one at a time, orthogonalised and as a step's weights:
+    the same bits, and nothing beside them."""
+    b, m, n = shape
+    x = matrix(8, *shape).to(DEV, torch.bfloat16)
+    p = R.muon_params()
+    ref = R.rft_orthogonalize(x, p)
+    w0 = matrix(18, *shape).to(DEV, torch.bfloat16)
+    wref = w0.clone()
+    R.rft_muon_step(wref, x, None, p)
+    for gap, first in ((0, 0), (8, 0), (4, 4), (1, 1)):
+        for step in (False, True):
+            buf = torch.full((b * m * (n + gap) + first,), math.nan, device=DEV, dtype=torch.bfloat16)
+            view = torch.as_strided(buf, shape, (m * (n + gap), n + gap, 1), first)
+            g = torch.empty_strided(shape, view.stride(), device=DEV, dtype=torch.bfloat16).copy_(x)
+            view.copy_(w0)
+            gaps = torch.isnan(buf)
+            if step:
+                R.rft_muon_step(view, g, None, p)
+            else:
+                R.rft_orthogonalize(g, p, out=view)
+            assert torch.equal(view, wref if step else ref)
+            assert torch.equal(torch.isnan(buf), gaps)
+
+
 def test_steps_coefficients_and_scale():
     x = matrix(3, 90, 140)
     for steps in (1, 2, 8):
