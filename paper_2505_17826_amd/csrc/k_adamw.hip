@@ -8,7 +8,7 @@
 // bytes of moments per element, the gradient, and the weight (and master) in and out.
 // Measured: 233 M elements, fp32 gradient, bf16 weight with a master: step 1318 us (7.0
 // GB, 5.3 TB/s; a copy of 1 GB reaches 5.2), norm 198 us (0.93 GB, 4.7 TB/s, a sum's
-// rate); 47 M elements with bf16 gradients 245 and 33 us.    Tensors come in batches of
+// rate); 47 M elements with bf16 gradients 245 and 33 us.  Tensors come in batches of
 // kMaxTensors per launch as kernel arguments; a block finds its tensor by its first
 // block's number.  Where every array of a tensor is 16-byte aligned (8 for bf16) a lane
 // takes four elements at a time; otherwise, and at a tensor's end, single elements.

@@ -184,7 +184,11 @@ def test_orthogonalize_workspace():
     size = lambda m, dt=R.RFT_F32, **kw: L.rft_orthogonalize_workspace_bytes(  # noqa: E731
         ctypes.byref(m), ctypes.byref(R.muon_params(**kw)), dt)
     one, three = size(_mats(), products=R.RFT_PRODUCTS_ONE), size(_mats(), products=R.RFT_PRODUCTS_THREE)
-    assert 0 < one < three == size(_mats()) and size(_mats(), R.RFT_BF16) == one
+    # up to 128 rows only X is in memory, as hi + lo for either kind of products
+    assert 0 < one <= three == size(_mats()) and size(_mats(), R.RFT_BF16) == one
+    big = _mats(rows=300, cols=700, rs=700)
+    assert size(big, products=R.RFT_PRODUCTS_ONE) < size(big, products=R.RFT_PRODUCTS_THREE) == size(big)
+    assert size(big, R.RFT_BF16) == size(big, products=R.RFT_PRODUCTS_ONE)
     assert size(_mats(batch=4)) > 3 * three
     # the orientation does not matter
     assert size(_mats(rows=300, cols=700, rs=700)) == size(_mats(rows=700, cols=300, rs=300))
