@@ -286,11 +286,13 @@ __device__ __forceinline__ void select(float (&key)[VPT], int l, int k, int& id)
   }
 }
 
-// exp(x - m) for x <= m, ml = m log2 e, by the hardware's exp2 (results below 2^-126 are
-// 0); x = -inf gives 0, NaN NaN.  The rounding of ml is a factor that all of a row's
-// values share (2^-24 |m|), that of the fma 2^-24 |x - m| of the value.
-__device__ __forceinline__ float exp_diff(float x, float ml) {
-  return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, -ml));
+// exp(x - m) for x <= m, m finite, by the hardware's exp2 (results below 2^-126 are 0);
+// x = -inf gives 0, NaN NaN.  The difference comes first: it is 0 at the maximum whatever
+// the logits' size, and its rounding and the product's are 2^-23 |x - m| of the value.
+// fma(x, log2 e, -m log2 e) would save an instruction per logit, but carries the rounding
+// of m log2 e, 2^-24 |m| in the exponent: a row of -1e9 is off by orders, one of -1e30 NaN.
+__device__ __forceinline__ float exp_diff(float x, float m) {
+  return __builtin_amdgcn_exp2f((x - m) * kLog2e);
 }
 
 template <int LPR, int VPT, bool BF16, bool STATS>
@@ -382,12 +384,12 @@ __global__ void __launch_bounds__(kThreads) k_router(
       }
       // the largest logit (or a NaN: the sums are NaN then)
       const float mx = unordered(group_max_u<LPR>(top));
-      const float m0 = mx < kExcluded ? 0.f : mx, ml = m0 * kLog2e;
+      const float m0 = mx < kExcluded ? 0.f : mx;
       float s = 0.f;
       float e[VPT];
 #pragma unroll
       for (int v = 0; v < VPT; ++v) {
-        e[v] = exp_diff(z[v], ml);
+        e[v] = exp_diff(z[v], m0);
         s += e[v];
       }
       s = group_sum<LPR>(s);
@@ -409,7 +411,7 @@ __global__ void __launch_bounds__(kThreads) k_router(
       if (l >= k || !was || (unsigned)id >= (unsigned)E) id = -1;
       if (id >= 0) {
         const float zi = look[id];
-        gate = exp_diff(zi, ml);
+        gate = exp_diff(zi, m0);
         if (zi < kExcluded) id = -1, gate = 0.f;
       }
       float den = rs;
@@ -813,12 +815,23 @@ __global__ void __launch_bounds__(kBwdThreads) k_router_bwd(
       }
     }
     const float ls = lse[t];
-    float p[VPT];
+    // p by the row's own maximum and sum: from lse, which is rounded to 2^-24 of itself, the
+    // p of a row of large logits would not add up to 1
+    float mx = z[0], s = 0.f, p[VPT];
+#pragma unroll
+    for (int v = 1; v < VPT; ++v) mx = fmaxf(mx, z[v]);
+    mx = group_max<LPR>(mx);
+    const float m0 = mx < kExcluded ? 0.f : mx;
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      p[v] = exp_diff(z[v], ls * kLog2e);
+      p[v] = exp_diff(z[v], m0);
+      s += p[v];
       d[v] = dp[v];
     }
+    s = group_sum<LPR>(s);
+    const float rs = s != 0.f ? __builtin_amdgcn_rcpf(s) : 0.f;
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) p[v] *= rs;
     if (d_gates) {
       // lane j holds place j and its gradient to the probability of its expert
       int id = -1;
@@ -832,7 +845,7 @@ __global__ void __launch_bounds__(kBwdThreads) k_router_bwd(
         float pe = 0.f;
         if (id >= 0)
           pe = exp_diff(BF16 ? bf16_to_f32(((const uint16_t*)row)[id]) : ((const float*)row)[id],
-                        ls * kLog2e);
+                        m0) * rs;
         const float sel = group_sum<LPR>(pe);
         const float mean = group_sum<LPR>(dg * pe);
         dg = id >= 0 && sel != 0.f ? (dg - mean / sel) / sel : 0.f;
