@@ -38,7 +38,15 @@ constexpr int kSumThreads = 1024, kSumWaves = kSumThreads / 64;
 // forward over more than 128 experts, 64 and fewer four, six, eight per SIMD), so that they
 // all run from start to end (8192 waves of which 6144 were resident: 52 us against 44).
 constexpr int64_t kSimds = 1024;
-inline int64_t fwd_waves(int E) { return kSimds * (E > 512 || (E > 128 && E <= 256) ? 4 : E > 64 ? 6 : 8); }
+// A wave adds up to kRowsInARow rows into one fp32 sum per expert before the sums are joined in
+// fp64 (an error of at most 2^-17 of a sum; the 43690 rows that a resident wave has of 2^30 gave
+// 4e-4); batches of more than 1-8 million rows take more waves for it.
+constexpr int64_t kRowsInARow = 256;
+inline int64_t fwd_waves(int64_t T, int E) {
+  const int64_t resident = kSimds * (E > 512 || (E > 128 && E <= 256) ? 4 : E > 64 ? 6 : 8);
+  const int64_t rows = kRowsInARow * (E <= 256 ? 4 : 1);
+  return std::max(resident, (T + rows - 1) / rows);
+}
 constexpr int64_t kBwdWaves = kSimds * 8;
 constexpr float kExcluded = -2e38f;     // logits below are excluded experts
 
@@ -893,10 +901,12 @@ Geom geometry(const rft_tokens& tok, const rft_router_params& p, const void* log
   return g;
 }
 
-// Groups with this many slots on average are summed by whole blocks per 16 experts.
-constexpr int64_t kManySlots = 16;
+// Groups with this many slots on average are summed by whole blocks per 16 experts, as long
+// as their number fits a grid.
+constexpr int64_t kManySlots = 16, kMaxSumBlocks = (int64_t)1 << 22;
 bool many_slots(const Geom& g, bool by_rollout) {
-  return !by_rollout || g.nW >= kManySlots * g.n_seq;
+  return !by_rollout || (g.nW >= kManySlots * g.n_seq &&
+                         (int64_t)g.n_seq * ((g.E + 15) / 16) <= kMaxSumBlocks);
 }
 int64_t sum_blocks(const Geom& g, bool by_rollout) {
   return many_slots(g, by_rollout) ? (int64_t)g.n_seq * ((g.E + 15) / 16)
@@ -970,7 +980,7 @@ extern "C" {
 size_t rft_router_workspace_bytes(const rft_tokens* tok, const rft_router_params* params) {
   if (check_router("rft_router_workspace_bytes", tok, params)) return 0;
   const Geom g = geometry(*tok, *params, nullptr, RFT_F32, params->n_experts,
-                          fwd_waves(params->n_experts));
+                          fwd_waves(tok->T, params->n_experts));
   Carver c(nullptr);
   carve(c, g, params->scope == RFT_BALANCE_ROLLOUT);
   return c.bytes();
@@ -991,8 +1001,9 @@ rft_status rft_router_fwd(const rft_tokens* tok, const void* logits, int dtype, 
     return fail(RFT_E_NULL, "%s: lse, counts, dprob and stats are given together, or counts, dprob "
                 "and stats not at all", fn);
   const bool by_rollout = params->scope == RFT_BALANCE_ROLLOUT;
-  const Geom g = geometry(*tok, *params, logits, dtype, ld, fwd_waves(params->n_experts));
-  if (sum_blocks(g, by_rollout) > ((int64_t)1 << 22))
+  const Geom g = geometry(*tok, *params, logits, dtype, ld,
+                          fwd_waves(tok->T, params->n_experts));
+  if (sum_blocks(g, by_rollout) > kMaxSumBlocks)
     return fail(RFT_E_SHAPE, "%s: n_seq=%lld is more than this many experts allow", fn,
                 (long long)tok->n_seq);
   Ws w = {};
