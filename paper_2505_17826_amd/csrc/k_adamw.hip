@@ -121,13 +121,15 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const double* part, int64
 }
 
 struct Hyper {
-  float decay, b1, c1, b2, c2, lr1, r2, eps;  // 1 - lr wd, beta1, 1 - beta1, ..., lr / bc1, 1 / sqrt(bc2)
+  float decay, b1, c1, b2, c2, lr1, r2, eps;  // lr wd, beta1, 1 - beta1, ..., lr / bc1, 1 / sqrt(bc2)
 };
 
 __device__ __forceinline__ float adamw1(float w, float g, float& m, float& v, const Hyper& h) {
   m = fmaf(h.b1, m, h.c1 * g);
   v = fmaf(h.b2, v, h.c2 * g * g);
-  return w * h.decay - h.lr1 * m / fmaf(sqrtf(v), h.r2, h.eps);
+  // the whole change before the weight's one rounding: 1 - lr wd in fp32 is 1 at lr wd = 1e-8,
+  // and 1 - 1.2e-7 at 1e-7
+  return w - fmaf(h.decay, w, h.lr1 * m / fmaf(sqrtf(v), h.r2, h.eps));
 }
 
 template <bool WB, bool GB, bool MASTER>
@@ -292,7 +294,7 @@ rft_status rft_adamw_step(const rft_param* params, int64_t n_params, int weight_
   const double bc1 = 1.0 - std::pow(p.beta1, p.step);
   const double bc2 = 1.0 - std::pow(p.beta2, p.step);
   Hyper h;
-  h.decay = (float)(1.0 - p.lr * p.weight_decay);
+  h.decay = (float)(p.lr * p.weight_decay);
   h.b1 = (float)p.beta1;
   h.c1 = (float)(1.0 - p.beta1);
   h.b2 = (float)p.beta2;
