@@ -45,3 +45,27 @@ def test_adamw(lr, wd, master, offset):
     assert abs(decay - want) <= limit(n, want) + 16 * 2.0 ** -24 * float(s.abs().mean()), (decay, want)
     if master:
         assert torch.equal(low, w.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("lr,wd", RATES)
+@pytest.mark.parametrize("master", [False, True])
+@pytest.mark.parametrize("shape", [(100, 8192), (8192, 99), (1024, 1024), (1023, 1025), (4, 400, 700),
+                                   (40, 300, 264)])
+def test_muon_step(lr, wd, master, shape):
+    n = math.prod(shape)
+    g = torch.Generator(DEV).manual_seed(9)
+    rows, cols = shape[-2:]
+    w = 1.0 + 2.0 ** -10 + torch.rand(shape, generator=g, device=DEV) * (1 - 2.0 ** -9)
+    u = torch.randn(shape, generator=g, device=DEV)
+    w0 = w.double()
+    low = w.to(torch.bfloat16)
+    scale = math.sqrt(max(rows, cols))  # entries of the update of lr in size: many fp32 steps
+    prm = lambda **kw: R.muon_params(products=R.RFT_PRODUCTS_THREE, **kw)  # noqa: E731
+    R.rft_muon_step(low if master else w, u, None, prm(lr=lr, weight_decay=wd, scale=scale),
+                    master=w if master else None)
+    s = lr * scale * R.rft_orthogonalize(u, prm()).double()
+    decay = float((w0 - s - w.double()).mean())
+    want = lr * wd * float(w0.mean())
+    assert abs(decay - want) <= limit(n, want) + 4 * 2.0 ** -24 * float(s.abs().mean()), (decay, want)
+    if master:
+        assert torch.equal(low, w.to(torch.bfloat16))
