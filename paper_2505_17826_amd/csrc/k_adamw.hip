@@ -293,6 +293,9 @@ rft_status rft_adamw_step(const rft_param* params, int64_t n_params, int weight_
   // factors in fp64: 1 - beta^step loses its digits in fp32 where beta is near 1
   const double bc1 = 1.0 - std::pow(p.beta1, p.step);
   const double bc2 = 1.0 - std::pow(p.beta2, p.step);
+  if (!(std::fabs(p.lr * p.weight_decay) <= 1e30) || !(std::fabs(p.lr / bc1) <= 1e30))
+    return fail(RFT_E_PARAM, "%s: lr=%g weight_decay=%g beta1=%g: a factor is past fp32", fn, p.lr,
+                p.weight_decay, p.beta1);
   Hyper h;
   h.decay = (float)(p.lr * p.weight_decay);
   h.b1 = (float)p.beta1;

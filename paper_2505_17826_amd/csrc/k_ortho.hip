@@ -1485,9 +1485,10 @@ rft_status rft_muon_step(const rft_matrices* mats, const void* grad, int grad_dt
   if (st) return st;
   if (!dtype_ok(grad_dtype) || !dtype_ok(weight_dtype))
     return fail(RFT_E_DTYPE, "%s: dtype %d / %d unknown", fn, grad_dtype, weight_dtype);
-  if (!fits(params->lr) || !fits(params->weight_decay))
-    return fail(RFT_E_PARAM, "%s: lr=%g weight_decay=%g", fn, params->lr,
-                params->weight_decay);
+  if (!fits(params->lr) || !fits(params->weight_decay) || !fits(params->lr * params->weight_decay) ||
+      !fits(params->lr * params->scale))
+    return fail(RFT_E_PARAM, "%s: lr=%g weight_decay=%g scale=%g", fn, params->lr,
+                params->weight_decay, params->scale);
   if (momentum_buf && !(params->momentum >= 0 && params->momentum < 1))
     return fail(RFT_E_PARAM, "%s: momentum=%g must be in [0, 1)", fn, params->momentum);
   if (master && weight_dtype != RFT_BF16)
