@@ -9,6 +9,8 @@ or no GPU is present the calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import math
 import os
 from dataclasses import dataclass
@@ -299,7 +301,49 @@ def _workspace(nbytes, device, ws=None):
     return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
 
 
+def _used_on(stream, *ts):
+    """Tells the allocator that arrays are used on a stream other than the one that they were
+    allocated on (they may be freed before its work is done)."""
+    if stream is not None:
+        for t in ts:
+            if t is not None and t.numel():
+                t.record_stream(stream)
+
+
+def _arrays(x):
+    """The tensors of an entry point's result."""
+    if isinstance(x, torch.Tensor):
+        return [x]
+    if isinstance(x, tuple):
+        return [t for y in x for t in _arrays(y)]
+    return [] if x is None else [t for y in vars(x).values() for t in _arrays(y)]
+
+
+def _allocates(f):
+    """An entry point that makes its workspace, or results that are not given.  With stream=
+    its body runs with that stream current, so that these are that stream's memory: a block
+    of the caller's current stream may have been freed by it with work still pending there,
+    and a fill there would not be ordered with the call.  The results then belong to the
+    caller, whose stream reads them: the allocator is told so."""
+    at = list(inspect.signature(f).parameters).index("stream")
+
+    @functools.wraps(f)
+    def call(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return f(*args, **kw)
+        callers = torch.cuda.current_stream(stream.device)
+        with torch.cuda.stream(stream):
+            out = f(*args, **kw)
+        if callers != stream:
+            _used_on(callers, *_arrays(out))
+        return out
+
+    return call
+
+
 # ------------------------------------------------------------ entry points --
+@_allocates
 def rft_group_advantages(rewards, group_size, eps=1e-6, out=None, stream=None, unbiased=True):
     _need_gpu(rewards)
     out = torch.empty_like(rewards) if out is None else out
@@ -309,6 +353,7 @@ def rft_group_advantages(rewards, group_size, eps=1e-6, out=None, stream=None, u
     return out
 
 
+@_allocates
 def rft_group_advantages_ids(rewards, group_id, n_groups, mode=RFT_ADV_GRPO, eps=1e-6, out=None,
                              stream=None, unbiased=True, ws=None):
     _need_gpu(rewards, group_id)
@@ -321,6 +366,7 @@ def rft_group_advantages_ids(rewards, group_id, n_groups, mode=RFT_ADV_GRPO, eps
     return out
 
 
+@_allocates
 def rft_token_logprobs(tokens: Tokens, hidden, weight, logp=None, entropy=None, lse=None, ws=None,
                        stream=None, want_entropy=True):
     _need_gpu(hidden, weight)
@@ -340,6 +386,7 @@ def rft_token_logprobs(tokens: Tokens, hidden, weight, logp=None, entropy=None, 
     return logp, entropy, lse
 
 
+@_allocates
 def rft_token_logprobs_from_logits(tokens: Tokens, logits, logp=None, entropy=None, lse=None,
                                    gathered=None, want_gathered=False, stream=None):
     _need_gpu(logits)
@@ -356,6 +403,7 @@ def rft_token_logprobs_from_logits(tokens: Tokens, logits, logp=None, entropy=No
     return logp, entropy, lse, gathered
 
 
+@_allocates
 def rft_ppo_clip_loss_fwd(tokens: Tokens, V, logp, old_logp, ref_logp, adv, params, entropy=None,
                           grad_logp=None, stats=None, ws=None, stream=None, grad_entropy=None):
     """Returns (grad_logp, stats); grad_entropy, when given, receives e_t."""
@@ -373,6 +421,7 @@ def rft_ppo_clip_loss_fwd(tokens: Tokens, V, logp, old_logp, ref_logp, adv, para
     return grad_logp, stats
 
 
+@_allocates
 def rft_ppo_clip_loss_bwd(tokens: Tokens, hidden, weight, lse, grad_logp, d_hidden=None,
                           d_weight=None, accumulate_dw=False, ws=None, stream=None,
                           grad_entropy=None, entropy=None):
@@ -392,6 +441,7 @@ def rft_ppo_clip_loss_bwd(tokens: Tokens, hidden, weight, lse, grad_logp, d_hidd
     return d_hidden, d_weight
 
 
+@_allocates
 def rft_ppo_clip_loss_bwd_logits(tokens: Tokens, logits, lse, grad_logp, d_logits=None,
                                  stream=None, grad_entropy=None, entropy=None):
     _need_gpu(logits, lse, grad_logp)
@@ -404,6 +454,7 @@ def rft_ppo_clip_loss_bwd_logits(tokens: Tokens, logits, lse, grad_logp, d_logit
     return d_logits
 
 
+@_allocates
 def rft_ppo_clip_fused_logits(tokens: Tokens, logits, old_logp, ref_logp, adv, params, logp=None,
                               entropy=None, lse=None, grad_logp=None, d_logits=None, stats=None,
                               ws=None, stream=None):
@@ -437,6 +488,7 @@ def rft_ppo_clip_fused_logits_noalloc(tokens: Tokens, logits, old_logp, ref_logp
     return logp, d_logits, stats
 
 
+@_allocates
 def rft_ppo_clip_step(tokens: Tokens, hidden, weight, old_logp, ref_logp, adv, params,
                       logp=None, entropy=None, lse=None, grad_logp=None, d_hidden=None,
                       d_weight=None, accumulate_dw=False, stats=None, ws=None, stream=None):
@@ -464,6 +516,7 @@ def rft_ppo_clip_step(tokens: Tokens, hidden, weight, old_logp, ref_logp, adv, p
     return logp, entropy, lse, grad_logp, d_hidden, d_weight, stats
 
 
+@_allocates
 def rft_sft_loss_fwd(tokens: Tokens, V, logp, agg=RFT_AGG_TOKEN_MEAN, denom_override=0.0,
                      grad_logp=None, stats=None, ws=None, stream=None):
     """Returns (grad_logp, stats)."""
@@ -478,6 +531,7 @@ def rft_sft_loss_fwd(tokens: Tokens, V, logp, agg=RFT_AGG_TOKEN_MEAN, denom_over
     return grad_logp, stats
 
 
+@_allocates
 def rft_dpo_loss_fwd(tokens: Tokens, V, logp, ref_logp, beta=0.1, label_smoothing=0.0,
                      grad_logp=None, seq_logp=None, want_seq_logp=True, stats=None, ws=None,
                      stream=None):
@@ -518,15 +572,6 @@ def _call(fn, device, stream, *args):
 
 def _at(t):
     return None if t is None else t.data_ptr()
-
-
-def _used_on(stream, *ts):
-    """Tells the allocator that arrays made here are used on a given stream, not on the
-    current one that they were allocated on (they may be freed before the work is done)."""
-    if stream is not None:
-        for t in ts:
-            if t is not None and t.numel():
-                t.record_stream(stream)
 
 
 def _want(dev, t, dtype, shape, name):
@@ -578,6 +623,7 @@ def _router_rows(T, x, E, name):
     return stride[0] if T > 1 else E
 
 
+@_allocates
 def rft_router_fwd(tokens: Tokens, logits, params, want_loss=True, out=None, ws=None, stream=None):
     """Returns a RouterOut; `out` (one of an earlier call with the same sizes) is written anew."""
     tk = tokens.c()
@@ -616,6 +662,7 @@ def rft_router_fwd(tokens: Tokens, logits, params, want_loss=True, out=None, ws=
     return out
 
 
+@_allocates
 def rft_router_bwd(tokens: Tokens, logits, params, fwd: RouterOut, d_gates=None, d_logits=None,
                    stream=None):
     """Returns d_logits; `fwd` is what rft_router_fwd returned for the same inputs."""
@@ -719,6 +766,7 @@ def _clip_at(dev, clip):
     return clip.buf.data_ptr()
 
 
+@_allocates
 def rft_grad_norm(params: Params, max_norm=0.0, clip=None, ws=None, stream=None) -> Clip:
     """Global gradient norm; the returned Clip feeds rft_adamw_step and rft_muon_step."""
     dev = params.device or torch.device("cuda", torch.cuda.current_device())
@@ -771,6 +819,7 @@ def _matrices(first, *others):
     return rft_matrices(b, r, c, *key(t))
 
 
+@_allocates
 def rft_orthogonalize(g, params, out=None, out_dtype=None, ws=None, stream=None):
     """Orthogonalises [rows, cols] or each of [batch, rows, cols]; out has g's strides."""
     _need_gpu(g, out)
@@ -788,6 +837,7 @@ def rft_orthogonalize(g, params, out=None, out_dtype=None, ws=None, stream=None)
     return out
 
 
+@_allocates
 def rft_muon_step(weight, grad, momentum, params, master=None, clip=None, ws=None, stream=None):
     """One orthogonalised momentum step in place; every array has the weight's strides."""
     _need_gpu(weight, grad, momentum, master)
