@@ -560,7 +560,12 @@ def _call(fn, device, stream, *args):
     the calls of a decode step take about as long on the host as on the GPU, so the device is
     set only where it is another one."""
     i = device.index
-    s = _raw_stream(i) if stream is None else stream.cuda_stream
+    if stream is None:
+        s = _raw_stream(i)
+    else:
+        if stream.device != device:
+            raise RuntimeError(f"stream is of {stream.device}, the call works on {device}")
+        s = stream.cuda_stream
     if torch.cuda.current_device() == i:
         st = fn(*args, s)
     else:
