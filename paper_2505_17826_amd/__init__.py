@@ -700,25 +700,41 @@ def rft_router_bwd(tokens: Tokens, logits, params, fwd: RouterOut, d_gates=None,
 
 
 # ----------------------------------------------------------------- updates --
+_data_ptr = torch.Tensor.data_ptr
+
+
 class Params:
     """Tensors of an update as (weight, grad, m, v[, master]) tuples, all contiguous and of one
     size each; a training program makes it once and keeps it.  For rft_grad_norm alone weight,
-    m and v may be None."""
+    m and v may be None.  A call uses the tensors where they lie when it is made (their storage
+    may have been replaced); where the gradient given was the weight's .grad, it takes the .grad
+    of that moment, which a backward pass may have made anew, and raises if there is none.
+    Other gradients are the tensors given: a program that makes them anew makes Params anew."""
 
     def __init__(self, tensors):
         self.tensors = [tuple(t) + (None,) * (5 - len(t)) for t in tensors]
         self.device = None
         self.weight_dtype = self.grad_dtype = None
         self.c = (rft_param * max(1, len(self.tensors)))()
-        f32 = torch.float32
+        self._follows = []  # tensors whose gradient is the weight's .grad
         for i, ts in enumerate(self.tensors):
             w, g = ts[:2]
             if self.device is None:
                 _need_gpu(g)
                 self.device, self.grad_dtype = g.device, g.dtype
-            if w is not None and self.weight_dtype is None:
-                self.weight_dtype = w.dtype
-            n = g.numel()
+            if w is not None:
+                if self.weight_dtype is None:
+                    self.weight_dtype = w.dtype
+                if w.requires_grad and w.is_leaf and w.grad is g:
+                    self._follows.append(i)
+        self._bind()
+
+    def _bind(self):
+        self._held = [t for ts in self.tensors for t in ts if t is not None]
+        self._ptrs = list(map(_data_ptr, self._held))
+        f32 = torch.float32
+        for i, ts in enumerate(self.tensors):
+            n = ts[1].numel()
             at = []
             for t, dt in zip(ts, (self.weight_dtype, self.grad_dtype, f32, f32, f32)):
                 if t is None:
@@ -731,6 +747,20 @@ class Params:
                                     f"{self.device} expected, got {t.dtype} {tuple(t.shape)} "
                                     f"on {t.device}")
             self.c[i] = (*at, n)
+
+    def now(self):
+        """The C list of the tensors as they are now."""
+        moved = False
+        for i in self._follows:
+            w, g, *rest = self.tensors[i]
+            if w.grad is not g:
+                if w.grad is None:
+                    raise RuntimeError(f"tensor {i}: the weight has no gradient")
+                self.tensors[i] = (w, w.grad, *rest)
+                moved = True
+        if moved or list(map(_data_ptr, self._held)) != self._ptrs:
+            self._bind()
+        return self.c
 
     def __len__(self):
         return len(self.tensors)
@@ -777,9 +807,9 @@ def rft_grad_norm(params: Params, max_norm=0.0, clip=None, ws=None, stream=None)
     dev = params.device or torch.device("cuda", torch.cuda.current_device())
     clip = Clip(dev) if clip is None else clip
     _same_device(dev, ("ws", ws))
-    L, n = lib(), len(params)
-    ws, nb = _workspace(int(L.rft_grad_norm_workspace_bytes(params.c, n)), dev, ws)
-    _call(L.rft_grad_norm, dev, stream, params.c, n, _code(params.grad_dtype), max_norm,
+    L, n, tensors = lib(), len(params), params.now()
+    ws, nb = _workspace(int(L.rft_grad_norm_workspace_bytes(tensors, n)), dev, ws)
+    _call(L.rft_grad_norm, dev, stream, tensors, n, _code(params.grad_dtype), max_norm,
           _clip_at(dev, clip), _at(ws), nb)
     _used_on(stream, clip.buf, ws)
     return clip
@@ -793,7 +823,7 @@ def adamw_params(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
 def rft_adamw_step(params: Params, hyper, clip=None, stream=None):
     """One AdamW step in place over every tensor of `params`."""
     dev = params.device or torch.device("cuda", torch.cuda.current_device())
-    _call(lib().rft_adamw_step, dev, stream, params.c, len(params), _code(params.weight_dtype),
+    _call(lib().rft_adamw_step, dev, stream, params.now(), len(params), _code(params.weight_dtype),
           _code(params.grad_dtype), ctypes.byref(hyper), _clip_at(dev, clip))
 
 
