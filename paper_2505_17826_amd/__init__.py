@@ -581,6 +581,8 @@ def _at(t):
 
 def _want(dev, t, dtype, shape, name):
     """A given array of a call: the dtype and shape that the entry point assumes, contiguous."""
+    if t is None:
+        raise TypeError(f"{name} is missing")
     if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise TypeError(f"{name}: contiguous {dtype} {tuple(shape)} expected, "
                         f"got {t.dtype} {tuple(t.shape)}")
