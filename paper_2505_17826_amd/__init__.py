@@ -13,6 +13,7 @@ import functools
 import inspect
 import math
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -304,10 +305,9 @@ def _workspace(nbytes, device, ws=None):
 def _used_on(stream, *ts):
     """Tells the allocator that arrays are used on a stream other than the one that they were
     allocated on (they may be freed before its work is done)."""
-    if stream is not None:
-        for t in ts:
-            if t is not None and t.numel():
-                t.record_stream(stream)
+    for t in ts:
+        if t is not None and t.numel():
+            t.record_stream(stream)
 
 
 def _arrays(x):
@@ -636,7 +636,10 @@ def rft_router_fwd(tokens: Tokens, logits, params, want_loss=True, out=None, ws=
     tk = tokens.c()
     dev, T, k, E = logits.device, tk.T, params.top_k, params.n_experts
     _need_gpu(logits)
-    _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start), ("ws", ws))
+    if not tokens.mask.device == dev == tokens.seq_start.device:
+        _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start))
+    if ws is not None:
+        _same_device(dev, ("ws", ws))
     dt, ld = _dtype_code(logits), _router_rows(T, logits, E, "logits")
     G = tk.n_seq if params.scope == RFT_BALANCE_ROLLOUT else 1
     i32, f32 = torch.int32, torch.float32
@@ -660,12 +663,14 @@ def rft_router_fwd(tokens: Tokens, logits, params, want_loss=True, out=None, ws=
     if not want_loss:
         _call(L.rft_router_fwd, dev, stream, rt, _at(logits), dt, ld, rp, _at(out.expert_ids),
               _at(out.gates), None, None, None, None, None, 0)
-        _used_on(stream, out.expert_ids, out.gates)
+        if stream is not None:
+            _used_on(stream, out.expert_ids, out.gates)
         return out
     ws, nb = _workspace(int(L.rft_router_workspace_bytes(rt, rp)), dev, ws)
     _call(L.rft_router_fwd, dev, stream, rt, _at(logits), dt, ld, rp, _at(out.expert_ids),
           _at(out.gates), _at(out.lse), _at(out.counts), _at(out.dprob), _at(out.stats), _at(ws), nb)
-    _used_on(stream, out.expert_ids, out.gates, out.lse, out.counts, out.dprob, out.stats, ws)
+    if stream is not None:
+        _used_on(stream, out.expert_ids, out.gates, out.lse, out.counts, out.dprob, out.stats, ws)
     return out
 
 
@@ -676,7 +681,8 @@ def rft_router_bwd(tokens: Tokens, logits, params, fwd: RouterOut, d_gates=None,
     tk = tokens.c()
     dev, T, k, E = logits.device, tk.T, params.top_k, params.n_experts
     _need_gpu(logits)
-    _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start))
+    if not tokens.mask.device == dev == tokens.seq_start.device:
+        _same_device(dev, ("mask", tokens.mask), ("seq_start", tokens.seq_start))
     dt, ld = _dtype_code(logits), _router_rows(T, logits, E, "logits")
     f32 = torch.float32
     if d_gates is not None:
@@ -697,12 +703,15 @@ def rft_router_bwd(tokens: Tokens, logits, params, fwd: RouterOut, d_gates=None,
     _call(lib().rft_router_bwd, dev, stream, ctypes.byref(tk), _at(logits), dt, ld,
           ctypes.byref(params), _at(fwd.expert_ids), _at(fwd.lse), _at(d_gates), _at(fwd.dprob),
           _at(fwd.stats), _at(d_logits), ldd)
-    _used_on(stream, d_logits)
+    if stream is not None:
+        _used_on(stream, d_logits)
     return d_logits
 
 
 # ----------------------------------------------------------------- updates --
 _data_ptr = torch.Tensor.data_ptr
+_PARAM = struct.Struct("5Qq")  # an rft_param
+_STATE_DTYPES = (torch.float32,) * 3  # of m, v and master
 
 
 class Params:
@@ -724,6 +733,7 @@ class Params:
             if self.device is None:
                 _need_gpu(g)
                 self.device, self.grad_dtype = g.device, g.dtype
+                self._index = g.get_device()
             if w is not None:
                 if self.weight_dtype is None:
                     self.weight_dtype = w.dtype
@@ -732,23 +742,25 @@ class Params:
         self._bind()
 
     def _bind(self):
-        self._held = [t for ts in self.tensors for t in ts if t is not None]
-        self._ptrs = list(map(_data_ptr, self._held))
-        f32 = torch.float32
+        held, ptrs = [], []
+        kinds = (self.weight_dtype, self.grad_dtype, *_STATE_DTYPES)
         for i, ts in enumerate(self.tensors):
-            n = ts[1].numel()
-            at = []
-            for t, dt in zip(ts, (self.weight_dtype, self.grad_dtype, f32, f32, f32)):
+            n, at = ts[1].numel(), []
+            for t, dt in zip(ts, kinds):
                 if t is None:
-                    at.append(None)
-                elif (t.dtype == dt and t.numel() == n and t.device == self.device
+                    at.append(0)
+                elif (t.dtype is dt and t.numel() == n and t.get_device() == self._index
                       and t.is_contiguous()):
-                    at.append(t.data_ptr())
+                    p = t.data_ptr()
+                    at.append(p)
+                    held.append(t)
+                    ptrs.append(p)
                 else:
                     raise TypeError(f"tensor {i}: contiguous {dt} of {n} elements on "
                                     f"{self.device} expected, got {t.dtype} {tuple(t.shape)} "
                                     f"on {t.device}")
-            self.c[i] = (*at, n)
+            _PARAM.pack_into(self.c, i * _PARAM.size, *at, n)
+        self._held, self._ptrs = held, ptrs
 
     def now(self):
         """The C list of the tensors as they are now."""
@@ -808,12 +820,14 @@ def rft_grad_norm(params: Params, max_norm=0.0, clip=None, ws=None, stream=None)
     """Global gradient norm; the returned Clip feeds rft_adamw_step and rft_muon_step."""
     dev = params.device or torch.device("cuda", torch.cuda.current_device())
     clip = Clip(dev) if clip is None else clip
-    _same_device(dev, ("ws", ws))
+    if ws is not None:
+        _same_device(dev, ("ws", ws))
     L, n, tensors = lib(), len(params), params.now()
     ws, nb = _workspace(int(L.rft_grad_norm_workspace_bytes(tensors, n)), dev, ws)
     _call(L.rft_grad_norm, dev, stream, tensors, n, _code(params.grad_dtype), max_norm,
           _clip_at(dev, clip), _at(ws), nb)
-    _used_on(stream, clip.buf, ws)
+    if stream is not None:
+        _used_on(stream, clip.buf, ws)
     return clip
 
 
@@ -870,7 +884,8 @@ def rft_orthogonalize(g, params, out=None, out_dtype=None, ws=None, stream=None)
     L, rm, rp = lib(), ctypes.byref(mats), ctypes.byref(params)
     ws, nb = _workspace(int(L.rft_orthogonalize_workspace_bytes(rm, rp, odt)), g.device, ws)
     _call(L.rft_orthogonalize, g.device, stream, rm, _at(g), dt, rp, _at(out), odt, _at(ws), nb)
-    _used_on(stream, out, ws)
+    if stream is not None:
+        _used_on(stream, out, ws)
     return out
 
 
@@ -890,7 +905,8 @@ def rft_muon_step(weight, grad, momentum, params, master=None, clip=None, ws=Non
     ws, nb = _workspace(need, dev, ws)
     _call(L.rft_muon_step, dev, stream, rm, _at(grad), gdt, _at(momentum), _at(weight), wdt,
           _at(master), rp, _clip_at(dev, clip), _at(ws), nb)
-    _used_on(stream, ws)
+    if stream is not None:
+        _used_on(stream, ws)
 
 
 def loaded_library_path() -> str:
