@@ -14,11 +14,16 @@
 //
 // Operands.  The matrix instructions take fp16 (11 significand bits, three more than
 // bf16, at the same rate; entries are bounded by the singular values, so fp16's range
-// is no limit).  Every matrix is kept as a sum of fp16 values hi + lo of kScale times
-// it (22 bits).  RFT_PRODUCTS_ONE multiplies the hi parts; X's own lo part enters as
-// p_i X_ij, so the iterate itself keeps 22 bits.  RFT_PRODUCTS_THREE adds hi lo and
-// lo hi (what is left out is 2^-22 of a product): errors as of fp32 products at three
-// times the instructions, where the card's fp32 instructions would take sixteen.
+// is no limit).  X is kept as a sum of fp16 values hi + lo of kScale times it (22 bits).
+// RFT_PRODUCTS_ONE multiplies the hi parts; X's own lo part enters as p_i X_ij, so the
+// iterate itself keeps 22 bits.  O and P are then hi alone (11 bits): the products read no
+// more of them, and the one place that could, b O, would gain little for another plane
+// (error of the result 5.9e-4 -> 5.8e-4 at 512 x 768, 3.7e-4 -> 3.0e-4 at 128 x 1536, in a
+// model of the arithmetic).  It is the choice for bf16 results, whose own rounding is
+// 1.65e-3: with it the error is 1.70e-3 to 1.76e-3, for a third of the instructions.
+// RFT_PRODUCTS_THREE keeps every matrix as hi + lo and adds the products hi lo and lo hi
+// (what is left out is 2^-22 of a product): errors as of fp32 products at three times
+// the instructions, where the card's fp32 instructions would take sixteen.
 //
 // Layout.  Operands are stored in blocks of 128 rows x 32 columns (8 KiB, row-major inside),
 // the blocks of a 128-row panel side by side, padded with zeros to multiples of 128 rows and

@@ -10,7 +10,7 @@
 //   k_router_sum  adds the slots of a group, 16 experts per block, 64 slots at a time:
 //                 counts, dprob and the loss terms; the last block writes the statistics
 //   k_router_sum_short  the same for many short rollouts: one wavefront per rollout
-//   k_router_bwd  d_logits: p is formed again from the logits and lse
+//   k_router_bwd  d_logits: p is formed again from the logits
 //
 // Slots (balance per rollout).  Wave w owns rows [w Rw, (w + 1) Rw); walking them, each
 // step to another rollout i or another wave raises w + i by one at least, so slot w + i
@@ -18,10 +18,10 @@
 // over its slots in a fixed order, so results are the same from run to run.
 //
 // Measured at 262144 rows (62% unmasked) x 128 fp32 experts, k = 8: forward 44 us (84 MB of
-// logits read, 17 MB written: its instructions bound it, about 420 vector instructions
-// per four rows, half of them the selection), sum 10.6 us (latency of two rounds of loads,
-// the reduction and the hand-over to the last block), backward 57 us (235 MB, 4.1 TB/s; a
-// large copy reaches 4.9-5.2 TB/s).
+// logits read, 18 MB written; 470 vector instructions per four rows, half of them the
+// selection, keep the SIMDs busy for 32 us of it, by counters), sum 10.8 us (latency of two
+// rounds of loads, the reduction and the hand-over to the last block), backward 55 us
+// (229 MB, 4.2 TB/s; a large copy reaches 4.8-5.2 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
