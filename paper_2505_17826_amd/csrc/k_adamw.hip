@@ -127,9 +127,7 @@ struct Hyper {
 __device__ __forceinline__ float adamw1(float w, float g, float& m, float& v, const Hyper& h) {
   m = fmaf(h.b1, m, h.c1 * g);
   v = fmaf(h.b2, v, h.c2 * g * g);
-  // the whole change before the weight's one rounding: 1 - lr wd in fp32 is 1 at lr wd = 1e-8,
-  // and 1 - 1.2e-7 at 1e-7
-  return w - fmaf(h.decay, w, h.lr1 * m / fmaf(sqrtf(v), h.r2, h.eps));
+  return stepped(w, h.decay, h.lr1 * m / fmaf(sqrtf(v), h.r2, h.eps));
 }
 
 template <bool WB, bool GB, bool MASTER>

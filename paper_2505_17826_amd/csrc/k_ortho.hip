@@ -74,9 +74,7 @@ struct Result {  // of LAST
   int64_t rows, cols, row_stride, batch_stride;
   void* out;     // rft_orthogonalize: out = scale X
   int out_bf16;
-  // rft_muon_step: w = w - (decay w + scale X), the whole change before the weight's one
-  // rounding: the factor 1 - lr wd in fp32 is 1 at lr wd = 1e-8, and 1 - 1.2e-7 at 1e-7
-  void* weight;
+  void* weight;  // rft_muon_step: w = w - (decay w + scale X)
   int weight_bf16;
   float* master;
   float decay, scale;
@@ -179,9 +177,6 @@ __device__ __forceinline__ floatx4 weights_at(const Result& r, int64_t at) {
   const u16x4 h = *(const u16x4*)((const uint16_t*)r.weight + at);
   return (floatx4){bf16_to_f32(h[0]), bf16_to_f32(h[1]), bf16_to_f32(h[2]), bf16_to_f32(h[3])};
 }
-__device__ __forceinline__ float stepped(const Result& r, float w, float y) {
-  return w - fmaf(r.decay, w, y);
-}
 // Eight bf16 elements at `at` (r.vec8): the weights there, and the result from y0, y1.
 __device__ __forceinline__ u16x8 weights8_at(const Result& r, int64_t at) {
   return *(const u16x8*)((const uint16_t*)r.weight + at);
@@ -191,7 +186,7 @@ __device__ __forceinline__ void result8_at(const Result& r, int64_t at, floatx4 
 #pragma unroll
   for (int q = 0; q < 8; ++q) {
     const float y = q < 4 ? y0[q & 3] : y1[q & 3];
-    z[q] = f32_to_bf16(r.weight ? stepped(r, bf16_to_f32(w[q]), y) : y);
+    z[q] = f32_to_bf16(r.weight ? stepped(bf16_to_f32(w[q]), r.decay, y) : y);
   }
   *(u16x8*)((uint16_t*)(r.weight ? r.weight : r.out) + at) = z;
 }
@@ -204,7 +199,8 @@ __device__ __forceinline__ void result_at(const Result& r, int64_t at, int64_t v
   const bool half = r.weight ? r.weight_bf16 : r.out_bf16;
   if (r.vec) {
     if (r.weight) {
-      y = w - fma4(r.decay, w, y);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] = stepped(w[q], r.decay, y[q]);
       if (r.master) *(floatx4*)(r.master + at) = y;
     }
     if (half)
@@ -222,7 +218,7 @@ __device__ __forceinline__ void result_at(const Result& r, int64_t at, int64_t v
       const float w0 = r.master ? r.master[at + q]
                        : r.weight_bf16 ? bf16_to_f32(((const uint16_t*)r.weight)[at + q])
                                        : ((const float*)r.weight)[at + q];
-      z = stepped(r, w0, z);
+      z = stepped(w0, r.decay, z);
       if (r.master) r.master[at + q] = z;
     }
     if (half)
