@@ -332,6 +332,9 @@ def _allocates(f):
         stream = args[at] if len(args) > at else kw.get("stream")
         if stream is None:
             return f(*args, **kw)
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor) and t.device != stream.device:
+                raise RuntimeError(f"an array is on {t.device}, stream is of {stream.device}")
         callers = torch.cuda.current_stream(stream.device)
         with torch.cuda.stream(stream):
             out = f(*args, **kw)

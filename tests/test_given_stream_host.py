@@ -13,8 +13,7 @@ import paper_2505_17826_amd as R
 
 class Stream:
     cuda_stream = 7
-    device = torch.device("cuda", 0)
-    device_index = 0
+    device = torch.device("cpu")  # of the arrays here
 
 
 @pytest.fixture
@@ -121,3 +120,12 @@ def test_without_a_stream_nothing_changes(spy, name):
     f(None)
     assert spy.allocated and all(s is spy.current for s in spy.allocated)
     assert not [s for s, _ in spy.recorded if s is not None]
+
+
+def test_a_stream_of_another_device_is_refused(spy):
+    side, x = Stream(), torch.zeros(2, device="meta")
+    with pytest.raises(RuntimeError, match="meta"):
+        R.rft_group_advantages(x, 2, stream=side)
+    with pytest.raises(RuntimeError, match="meta"):
+        R.rft_group_advantages(torch.zeros(2), 2, out=x, stream=side)
+    assert not spy.called
