@@ -517,8 +517,8 @@ rft_status rft_router_fwd(const rft_tokens* tok, const void* logits, int dtype, 
  *   g_e = c_b / n_groups dprob_e + [e selected at j] s_j,
  *   d_logits_e = p_e (g_e - sum_i p_i g_i) + 2 c_z lse / n_valid p_e.
  * logits, expert_ids, lse (read in the last term alone), dprob and stats as the
- * forward had and wrote them (ids outside [0, E) are places without an expert).  d_logits [T, E] in `dtype`,
- * rows ldd elements apart; masked rows and excluded experts get 0.  d_logits may be
+ * forward had and wrote them (ids outside [0, E) are places without an expert).
+ * d_logits [T, E] in `dtype`, rows ldd elements apart; masked rows and excluded experts get 0.  d_logits may be
  * logits itself.  Errors: as rft_router_fwd. */
 rft_status rft_router_bwd(const rft_tokens* tok, const void* logits, int dtype, int64_t ld,
                           const rft_router_params* params, const int32_t* expert_ids,
@@ -549,7 +549,8 @@ typedef struct {
 /* Global 2-norm of the gradients of n_params tensors (params: host array; only
  * grad and n are read), summed in fp64 in a fixed order.  max_norm = 0: no
  * clipping.  One call takes gradients of one type; of two types the caller joins two
- * norms a and b and writes an rft_clip from sqrt(a^2 + b^2).  Workspace: rft_grad_norm_workspace_bytes().
+ * norms a and b and writes an rft_clip from sqrt(a^2 + b^2).
+ * Workspace: rft_grad_norm_workspace_bytes().
  * Errors: RFT_E_NULL, RFT_E_SHAPE, RFT_E_DTYPE, RFT_E_PARAM, RFT_E_WORKSPACE. */
 size_t rft_grad_norm_workspace_bytes(const rft_param* params, int64_t n_params);
 rft_status rft_grad_norm(const rft_param* params, int64_t n_params, int grad_dtype,
@@ -628,7 +629,7 @@ rft_status rft_orthogonalize(const rft_matrices* mats, const void* g, int dtype,
  * with w the master (fp32) where given, else the weight in its own type, and the
  * weight then the rounding of the master.  momentum_buf f32; NULL: u = grad (and
  * momentum is ignored).  clip (device, may be NULL): grad is scaled by clip->scale
- * first, and with clip->finite == 0 nothing changes.
+ * first, and with clip->finite == 0 nothing changes.  The arrays may not overlap.
  * Workspace: rft_orthogonalize_workspace_bytes() with out_dtype RFT_F32 when a
  * master is given, else the weight's.
  * Errors: as rft_orthogonalize. */
