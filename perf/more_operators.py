@@ -83,7 +83,7 @@ def draw(rng):
         E, d = _log(rng, 4, 512), step * _log(rng, 64 // step, 4096 // step)
         k = min(E, _log(rng, 1, 10))
         train = rng.random() < 0.6
-        most = int(1.0e9) // (d * k * (2 if dtype == "bf16" else 4))
+        most = int(8.0e8) // (d * k * (2 if dtype == "bf16" else 4))
         rows = max(1, min(_log(rng, 1, 131072 if train else 4096), most))
         pad = min(rows, _log(rng, 1, 2048)) if train else 1
         c = _tokens("", train=train, dtype=dtype, n_seq=max(1, rows // pad),
