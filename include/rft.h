@@ -57,7 +57,7 @@
 extern "C" {
 #endif
 
-#define RFT_ABI_VERSION 8
+#define RFT_ABI_VERSION 9
 
 typedef enum {
   RFT_OK = 0,
@@ -637,6 +637,122 @@ rft_status rft_muon_step(const rft_matrices* mats, const void* grad, int grad_dt
                          float* momentum_buf, void* weight, int weight_dtype, float* master,
                          const rft_muon_params* params, const rft_clip* clip, void* ws,
                          size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ experts --
+ * What lies between the router and the sum of its experts: the tokens' slots in
+ * the order of their experts, the experts' products over their rows, and the way
+ * back to the tokens, each with its gradient.  A layer of experts is
+ *   rft_router_fwd -> rft_expert_sort -> rft_linear (up, from the tokens' rows)
+ *   -> rft_linear (down) -> rft_expert_combine,
+ * and its backward rft_expert_combine_bwd -> rft_linear_bwd (down, up)
+ * -> rft_expert_combine (no gates) -> rft_router_bwd. */
+
+/* (host struct holding device pointers) The T top_k slots of a batch (slot
+ * t top_k + j is place j of token t) in the order of their experts, as
+ * rft_expert_sort writes it.  n = offsets[n_experts] slots have an expert. */
+typedef struct {
+  int64_t T;
+  int32_t top_k;      /* k, 1 <= k <= 16                                          */
+  int32_t n_experts;  /* E, 1 <= E <= 1024                                        */
+  int32_t* offsets;   /* [E + 1] expert e has sorted rows [offsets[e], offsets[e+1]) */
+  int32_t* slots;     /* [T k] slot of a sorted row; -1 from row n on             */
+  int32_t* places;    /* [T, k] sorted row of a slot; -1 for one without an expert */
+} rft_expert_order;
+
+/* Slots sorted by expert, those of one expert in ascending order.  expert_ids
+ * [T, k] int32, as rft_router_fwd writes them: an id outside [0, E) is a slot
+ * without an expert; a token may name an expert twice.  T k < 2^31.
+ * Workspace: rft_expert_sort_workspace_bytes() (0 for small batches).
+ * Errors: RFT_E_NULL, RFT_E_SHAPE, RFT_E_WORKSPACE. */
+size_t rft_expert_sort_workspace_bytes(int64_t T, int32_t top_k, int32_t n_experts);
+rft_status rft_expert_sort(const int32_t* expert_ids, const rft_expert_order* order, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* The tokens' rows in sorted order: rows[r] = gates[s] x[s div k], s = slots[r]
+ * (gates [T, k] f32, or NULL: the rows themselves).  x [T, d], rows [T k, d] in
+ * `dtype`, any alignment of it; rows from n on are left as they were.  The
+ * gradient to x is rft_expert_combine of the rows' gradient, with the same gates.
+ * In this call and the next two, the order's arrays are read, those of another
+ * batch give unspecified values within the arrays given; gates are rounded nowhere.
+ * Errors: RFT_E_NULL, RFT_E_SHAPE, RFT_E_DTYPE. */
+rft_status rft_expert_gather(const rft_expert_order* order, const void* x, int dtype, int64_t d,
+                             const float* gates, void* rows, void* stream);
+
+/* The rows of each token's experts summed:
+ *   out[t] = residual[t] + sum_j gates[t, j] rows[places[t, j]]
+ * in fp32, j ascending, rounded once; slots without an expert add nothing
+ * whatever their gate.  gates NULL: 1; residual [T, d] NULL: 0.  rows [T k, d],
+ * out [T, d] in `dtype`; out may be residual.  Errors: as rft_expert_gather. */
+rft_status rft_expert_combine(const rft_expert_order* order, const void* rows, int dtype, int64_t d,
+                              const float* gates, const void* residual, void* out, void* stream);
+
+/* Gradients of rft_expert_combine (that of the residual is d_out itself):
+ *   d_rows[r] = gates[s] d_out[s div k], s = slots[r] (left as it was from n on),
+ *   d_gates[t, j] = <d_out[t], rows[places[t, j]]>, 0 without an expert,
+ * sums in fp32.  d_rows may be rows itself; d_rows or d_gates may be NULL (rows
+ * is then needed for d_gates alone).  Errors: as rft_expert_gather. */
+rft_status rft_expert_combine_bwd(const rft_expert_order* order, const void* d_out, const void* rows,
+                                  int dtype, int64_t d, const float* gates, void* d_rows,
+                                  float* d_gates, void* stream);
+
+/* Activations in the epilogue of a product.  RFT_ACT_SWIGLU halves the columns:
+ * z = [g | u] (n even), silu(g) u. */
+typedef enum { RFT_ACT_NONE = 0, RFT_ACT_SILU = 1, RFT_ACT_GELU = 2, RFT_ACT_SWIGLU = 3 } rft_act;
+
+/* (host struct holding device pointers) The rows of a product and whose weight
+ * each takes: group g (an expert) has rows [offsets[g], offsets[g+1]).  Rows from
+ * offsets[n_groups] on belong to none: they are neither read nor written.  offsets
+ * NULL: one group of all rows.  offsets are taken as non-decreasing and inside
+ * [0, rows]; others give unspecified values, every access stays in bounds.
+ * With source (e.g. an order's slots, and source_div its top_k), row r of x is
+ * x[source[r] div source_div], and x has source_rows rows; a source outside them
+ * is a row of zeros.  Without, x has `rows` rows. */
+typedef struct {
+  int64_t rows;            /* < 2^31                                               */
+  int32_t n_groups;        /* 1 .. 1024                                            */
+  const int32_t* offsets;  /* [n_groups + 1], or NULL (n_groups 1)                 */
+  const int32_t* source;   /* [rows], or NULL                                      */
+  int32_t source_div;      /* >= 1; read only with source                          */
+  int64_t source_rows;     /* read only with source                                */
+} rft_groups;
+
+/* Linear layer of every group, its bias, activation and residual in one pass:
+ *   z[r] = weight_g x[r] + bias_g,  y[r] = act(z[r]) + residual[r].
+ * x [rows or source_rows, k], weight [n_groups, n, k], bias [n_groups, n] or NULL,
+ * residual and y [rows, m] (m = n, or n / 2 with RFT_ACT_SWIGLU; residual may be
+ * NULL or y), z [rows, n] or NULL: kept for the backward, all in `dtype`.  fp32 sums;
+ * y and z are each rounded once from them (bf16: products by matrix instructions,
+ * fp32 arithmetic in fp32).  RFT_ACT_GELU is z Phi(z).
+ * bf16 needs k % 8 == 0, n % 8 == 0 (n % 16 with RFT_ACT_SWIGLU), 16-byte aligned
+ * arrays and, with source, source_rows k < 2^31 - 64; fp32 takes any sizes and
+ * alignments.  n k < 2^31 - 64.
+ * Workspace: rft_linear_workspace_bytes().
+ * Errors: RFT_E_NULL, RFT_E_SHAPE, RFT_E_DTYPE, RFT_E_PARAM, RFT_E_WORKSPACE. */
+size_t rft_linear_workspace_bytes(const rft_groups* groups, int dtype, int64_t k, int64_t n,
+                                  int32_t act);
+rft_status rft_linear(const rft_groups* groups, const void* x, const void* weight, int dtype,
+                      int64_t k, int64_t n, const void* bias, int32_t act, const void* residual,
+                      void* y, void* z, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of rft_linear (that of the residual is dy itself):
+ *   dz = dy act'(z), d_x[r] = dz[r] weight_g, d_weight_g = sum_r dz[r]^T x[r],
+ *   d_bias_g = sum_r dz[r].
+ * dy [rows, m] and z [rows, n] (as rft_linear wrote it; NULL with RFT_ACT_NONE) in
+ * `dtype`; groups, x and weight as there.  d_x [rows, k] in `dtype`: with source
+ * too it has the groups' rows (rft_expert_combine sums those of a token); d_weight
+ * [n_groups, n, k] in dw_dtype (RFT_F32 or `dtype`), d_bias [n_groups, n] f32; each
+ * may be NULL.  accumulate != 0: d_weight (RFT_F32) and d_bias are added to; a group
+ * without rows has zeros (adds nothing).  With bf16 data the products take dz in
+ * bf16 (with RFT_ACT_NONE that is dy itself); d_bias sums it unrounded.
+ * Sums run in a fixed order.
+ * Workspace: rft_linear_bwd_workspace_bytes().
+ * Errors: as rft_linear. */
+size_t rft_linear_bwd_workspace_bytes(const rft_groups* groups, int dtype, int64_t k, int64_t n,
+                                      int32_t act);
+rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* z, const void* x,
+                          const void* weight, int dtype, int64_t k, int64_t n, int32_t act,
+                          void* d_x, void* d_weight, int dw_dtype, float* d_bias,
+                          int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

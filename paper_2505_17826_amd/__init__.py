@@ -27,6 +27,7 @@ RFT_F32, RFT_BF16 = 0, 1
 RFT_AGG_SEQ_MEAN_TOKEN_MEAN, RFT_AGG_TOKEN_MEAN = 0, 1
 RFT_ADV_GRPO, RFT_ADV_MEAN_CENTER, RFT_ADV_LEAVE_ONE_OUT = 0, 1, 2
 RFT_BALANCE_BATCH, RFT_BALANCE_ROLLOUT = 0, 1
+RFT_ACT_NONE, RFT_ACT_SILU, RFT_ACT_GELU, RFT_ACT_SWIGLU = range(4)
 RFT_PRODUCTS_BY_TYPE, RFT_PRODUCTS_ONE, RFT_PRODUCTS_THREE = 0, 1, 3
 (RFT_OP_TOKEN_LOGPROBS, RFT_OP_TOKEN_LOGPROBS_FROM_LOGITS, RFT_OP_PPO_FWD, RFT_OP_PPO_BWD,
  RFT_OP_PPO_BWD_LOGITS, RFT_OP_PPO_FUSED_LOGITS, RFT_OP_PPO_STEP, RFT_OP_SFT_FWD,
@@ -103,6 +104,16 @@ class rft_muon_params(ctypes.Structure):
                 ("products", ctypes.c_int32)]
 
 
+class rft_expert_order(ctypes.Structure):
+    _fields_ = [("T", _i64), ("top_k", ctypes.c_int32), ("n_experts", ctypes.c_int32),
+                ("offsets", _p), ("slots", _p), ("places", _p)]
+
+
+class rft_groups(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("n_groups", ctypes.c_int32), ("offsets", _p), ("source", _p),
+                ("source_div", ctypes.c_int32), ("source_rows", _i64)]
+
+
 STATS_BYTES = ctypes.sizeof(rft_ppo_stats)
 DPO_STATS_BYTES = ctypes.sizeof(rft_dpo_stats)
 
@@ -172,6 +183,24 @@ _SIGS = {
     "rft_muon_step": (ctypes.c_int, [ctypes.POINTER(rft_matrices), _p, ctypes.c_int, _p, _p,
                                      ctypes.c_int, _p, ctypes.POINTER(rft_muon_params), _p, _p,
                                      ctypes.c_size_t, _p]),
+    "rft_expert_sort_workspace_bytes": (ctypes.c_size_t, [_i64, ctypes.c_int32, ctypes.c_int32]),
+    "rft_expert_sort": (ctypes.c_int, [_p, ctypes.POINTER(rft_expert_order), _p, ctypes.c_size_t,
+                                       _p]),
+    "rft_expert_gather": (ctypes.c_int, [ctypes.POINTER(rft_expert_order), _p, ctypes.c_int, _i64,
+                                         _p, _p, _p]),
+    "rft_expert_combine": (ctypes.c_int, [ctypes.POINTER(rft_expert_order), _p, ctypes.c_int, _i64,
+                                          _p, _p, _p, _p]),
+    "rft_expert_combine_bwd": (ctypes.c_int, [ctypes.POINTER(rft_expert_order), _p, _p, ctypes.c_int,
+                                              _i64, _p, _p, _p, _p]),
+    "rft_linear_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(rft_groups), ctypes.c_int, _i64,
+                                                     _i64, ctypes.c_int32]),
+    "rft_linear": (ctypes.c_int, [ctypes.POINTER(rft_groups), _p, _p, ctypes.c_int, _i64, _i64, _p,
+                                  ctypes.c_int32, _p, _p, _p, _p, ctypes.c_size_t, _p]),
+    "rft_linear_bwd_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(rft_groups), ctypes.c_int,
+                                                         _i64, _i64, ctypes.c_int32]),
+    "rft_linear_bwd": (ctypes.c_int, [ctypes.POINTER(rft_groups), _p, _p, _p, _p, ctypes.c_int, _i64,
+                                      _i64, ctypes.c_int32, _p, _p, ctypes.c_int, _p, ctypes.c_int32,
+                                      _p, ctypes.c_size_t, _p]),
 }
 
 _LIB = None
@@ -910,6 +939,232 @@ def rft_muon_step(weight, grad, momentum, params, master=None, clip=None, ws=Non
           _at(master), rp, _clip_at(dev, clip), _at(ws), nb)
     if stream is not None:
         _used_on(stream, ws)
+
+
+# ----------------------------------------------------------------- experts --
+@dataclass
+class ExpertOrder:
+    """Slots of a batch in the order of their experts, as rft_expert_sort returns it."""
+    offsets: torch.Tensor  # int32 [E + 1]
+    slots: torch.Tensor    # int32 [T * k]
+    places: torch.Tensor   # int32 [T, k]
+
+    @property
+    def n_experts(self):
+        return int(self.offsets.numel()) - 1
+
+    def c(self) -> rft_expert_order:
+        if self.places.dim() != 2:
+            raise TypeError("places: int32 [T, k] expected")
+        dev, (T, k) = self.places.device, self.places.shape
+        _want(dev, self.places, torch.int32, (T, k), "places")
+        _want(dev, self.slots, torch.int32, (T * k,), "slots")
+        _want(dev, self.offsets, torch.int32, (self.offsets.numel(),), "offsets")
+        return rft_expert_order(T, k, self.n_experts, _at(self.offsets), _at(self.slots),
+                                _at(self.places))
+
+    def groups(self, gather=False):
+        """The rows of an rft_linear over the experts; gather: its x are the tokens' rows."""
+        return Groups(self.offsets, self.slots if gather else None, self.places.shape[1])
+
+
+@dataclass
+class Groups:
+    """Rows of a product and whose weight each takes: group g has rows [offsets[g],
+    offsets[g + 1]).  With source, row r of x is x[source[r] // source_div]."""
+    offsets: torch.Tensor         # int32 [E + 1]
+    source: torch.Tensor = None   # int32 [rows]
+    source_div: int = 1
+
+
+@_allocates
+def rft_expert_sort(expert_ids, n_experts, out=None, ws=None, stream=None) -> ExpertOrder:
+    """Sorts the slots of expert_ids [T, k] (int32; outside [0, n_experts): none) by expert;
+    `out` (of an earlier call with the same sizes) is written anew."""
+    _need_gpu(expert_ids)
+    dev = expert_ids.device
+    if expert_ids.dim() != 2:
+        raise TypeError("expert_ids: int32 [T, k] expected")
+    T, k = expert_ids.shape
+    _want(dev, expert_ids, torch.int32, (T, k), "expert_ids")
+    _same_device(dev, ("ws", ws))
+    if out is None:
+        new = functools.partial(torch.empty, dtype=torch.int32, device=dev)
+        out = ExpertOrder(new(max(0, n_experts) + 1), new(T * k), new((T, k)))
+    else:
+        _want(dev, out.offsets, torch.int32, (n_experts + 1,), "offsets")
+        _want(dev, out.slots, torch.int32, (T * k,), "slots")
+        _want(dev, out.places, torch.int32, (T, k), "places")
+    L = lib()
+    o = rft_expert_order(T, k, n_experts, _at(out.offsets), _at(out.slots), _at(out.places))
+    ws, nb = _workspace(int(L.rft_expert_sort_workspace_bytes(T, k, n_experts)), dev, ws)
+    _call(L.rft_expert_sort, dev, stream, _at(expert_ids), ctypes.byref(o), _at(ws), nb)
+    if stream is not None:
+        _used_on(stream, out.offsets, out.slots, out.places, ws)
+    return out
+
+
+def _expert_rows(order, named, d):
+    """The order as a C struct, with the arrays of a call checked: (name, tensor, rows)."""
+    o = order.c()
+    dev = order.places.device
+    first = next(t for _, t, _ in named if t is not None)
+    for name, t, rows in named:
+        if t is not None:
+            _want(dev, t, first.dtype, (rows, d), name)
+    return o, dev, _dtype_code(first)
+
+
+def _gates(order, gates, dev):
+    if gates is not None:
+        _want(dev, gates, torch.float32, tuple(order.places.shape), "gates")
+    return _at(gates)
+
+
+@_allocates
+def rft_expert_gather(order: ExpertOrder, x, gates=None, out=None, stream=None):
+    """Returns [T k, d]: the tokens' rows in the order of their experts (times their gates); rows
+    from offsets[E] on are left as they were.  Its gradient is rft_expert_combine."""
+    _need_gpu(x)
+    T, k = order.places.shape
+    d = x.shape[-1]
+    if out is None:
+        out = torch.empty((T * k, d), dtype=x.dtype, device=x.device)
+    o, dev, dt = _expert_rows(order, (("x", x, T), ("out", out, T * k)), d)
+    _call(lib().rft_expert_gather, dev, stream, ctypes.byref(o), _at(x), dt, d,
+          _gates(order, gates, dev), _at(out))
+    if stream is not None:
+        _used_on(stream, out)
+    return out
+
+
+@_allocates
+def rft_expert_combine(order: ExpertOrder, rows, gates=None, residual=None, out=None, stream=None):
+    """Returns [T, d]: the sum of each token's rows (times their gates), and of the residual."""
+    _need_gpu(rows)
+    T, k = order.places.shape
+    d = rows.shape[-1]
+    if out is None:
+        out = torch.empty((T, d), dtype=rows.dtype, device=rows.device)
+    o, dev, dt = _expert_rows(order, (("rows", rows, T * k), ("residual", residual, T),
+                                      ("out", out, T)), d)
+    _call(lib().rft_expert_combine, dev, stream, ctypes.byref(o), _at(rows), dt, d,
+          _gates(order, gates, dev), _at(residual), _at(out))
+    if stream is not None:
+        _used_on(stream, out)
+    return out
+
+
+@_allocates
+def rft_expert_combine_bwd(order: ExpertOrder, d_out, rows, gates=None, d_rows=None, d_gates=None,
+                           want_d_rows=True, want_d_gates=True, stream=None):
+    """Returns (d_rows, d_gates); d_rows (which may be rows) is left as it was from offsets[E]
+    on.  rows may be None without d_gates."""
+    _need_gpu(d_out)
+    T, k = order.places.shape
+    d = d_out.shape[-1]
+    if d_rows is None and want_d_rows:
+        d_rows = torch.empty((T * k, d), dtype=d_out.dtype, device=d_out.device)
+    if d_gates is None and want_d_gates:
+        d_gates = torch.empty((T, k), dtype=torch.float32, device=d_out.device)
+    o, dev, dt = _expert_rows(order, (("d_out", d_out, T), ("rows", rows, T * k),
+                                      ("d_rows", d_rows, T * k)), d)
+    if d_gates is not None:
+        _want(dev, d_gates, torch.float32, (T, k), "d_gates")
+    _call(lib().rft_expert_combine_bwd, dev, stream, ctypes.byref(o), _at(d_out), _at(rows), dt, d,
+          _gates(order, gates, dev), _at(d_rows), _at(d_gates))
+    if stream is not None:
+        _used_on(stream, d_rows, d_gates)
+    return d_rows, d_gates
+
+
+def _linear_groups(groups, x, weight):
+    """(C struct, rows, E, n, k) of a linear layer; weight [E, n, k], or [n, k] for one group."""
+    dev = x.device
+    if weight.dim() not in (2, 3) or x.dim() != 2:
+        raise TypeError("x: [rows, k], weight: [groups, n, k] or [n, k] expected")
+    E = weight.shape[0] if weight.dim() == 3 else 1
+    n, k = weight.shape[-2:]
+    _want(dev, x, weight.dtype, (x.shape[0], k), "x")
+    _want(dev, weight, weight.dtype, tuple(weight.shape), "weight")
+    rows = x.shape[0]
+    if groups is None:
+        return rft_groups(rows, E, None, None, 1, 0), rows, E, n, k
+    _want(dev, groups.offsets, torch.int32, (E + 1,), "offsets")
+    src = groups.source
+    if src is not None:
+        rows = src.numel()
+        _want(dev, src, torch.int32, (rows,), "source")
+    return rft_groups(rows, E, _at(groups.offsets), _at(src), groups.source_div,
+                      x.shape[0]), rows, E, n, k
+
+
+@_allocates
+def rft_linear(x, weight, bias=None, act=RFT_ACT_NONE, residual=None, groups: Groups = None,
+               want_z=False, out=None, z=None, ws=None, stream=None):
+    """Returns (y, z): y = act(x weight^T + bias) + residual, z what act takes (None unless
+    wanted).  weight [n, k] with x [rows, k]; or weight [E, n, k] with groups (rows of no group
+    are left as they were)."""
+    _need_gpu(x, weight)
+    g, rows, E, n, k = _linear_groups(groups, x, weight)
+    dev, dt = x.device, _dtype_code(x)
+    m = n // 2 if act == RFT_ACT_SWIGLU else n
+    if bias is not None:
+        _want(dev, bias, x.dtype, tuple(weight.shape[:-1]), "bias")
+    out = torch.empty((rows, m), dtype=x.dtype, device=dev) if out is None else out
+    if z is None and want_z:
+        z = torch.empty((rows, n), dtype=x.dtype, device=dev)
+    for name, t, c in (("residual", residual, m), ("out", out, m), ("z", z, n)):
+        if t is not None:
+            _want(dev, t, x.dtype, (rows, c), name)
+    _same_device(dev, ("ws", ws))
+    L, rg = lib(), ctypes.byref(g)
+    ws, nb = _workspace(int(L.rft_linear_workspace_bytes(rg, dt, k, n, act)), dev, ws)
+    _call(L.rft_linear, dev, stream, rg, _at(x), _at(weight), dt, k, n, _at(bias), act,
+          _at(residual), _at(out), _at(z), _at(ws), nb)
+    if stream is not None:
+        _used_on(stream, out, z, ws)
+    return out, z
+
+
+@_allocates
+def rft_linear_bwd(dy, x, weight, z=None, act=RFT_ACT_NONE, groups: Groups = None, want_dx=True,
+                   want_dw=True, want_db=False, d_x=None, d_weight=None, d_bias=None, dw_dtype=None,
+                   accumulate=False, ws=None, stream=None):
+    """Returns (d_x, d_weight, d_bias), None where not wanted.  d_weight has dw_dtype (default:
+    the weight's), d_bias is fp32; accumulate adds to the d_weight (fp32) and d_bias given.  With
+    groups.source d_x has the groups' rows; rft_expert_combine sums those of a token."""
+    _need_gpu(dy, x, weight)
+    g, rows, E, n, k = _linear_groups(groups, x, weight)
+    dev, dt = x.device, _dtype_code(x)
+    m = n // 2 if act == RFT_ACT_SWIGLU else n
+    if accumulate and ((want_dw and d_weight is None) or (want_db and d_bias is None)):
+        raise TypeError("accumulate adds to the d_weight and d_bias given")
+    if d_x is None and want_dx:
+        d_x = torch.empty((rows, k), dtype=x.dtype, device=dev)
+    if d_weight is None and want_dw:
+        d_weight = torch.empty(weight.shape, dtype=dw_dtype or weight.dtype, device=dev)
+    if d_bias is None and want_db:
+        d_bias = torch.empty(weight.shape[:-1], dtype=torch.float32, device=dev)
+    for name, t, c in (("dy", dy, m), ("z", z, n), ("d_x", d_x, k)):
+        if t is not None:
+            _want(dev, t, x.dtype, (rows, c), name)
+    dwt = dt
+    if d_weight is not None:
+        if dw_dtype is not None and d_weight.dtype != dw_dtype:
+            raise TypeError("d_weight has another dtype than dw_dtype")
+        _want(dev, d_weight, d_weight.dtype, tuple(weight.shape), "d_weight")
+        dwt = _dtype_code(d_weight)
+    if d_bias is not None:
+        _want(dev, d_bias, torch.float32, tuple(weight.shape[:-1]), "d_bias")
+    _same_device(dev, ("ws", ws))
+    L, rg = lib(), ctypes.byref(g)
+    ws, nb = _workspace(int(L.rft_linear_bwd_workspace_bytes(rg, dt, k, n, act)), dev, ws)
+    _call(L.rft_linear_bwd, dev, stream, rg, _at(dy), _at(z), _at(x), _at(weight), dt, k, n, act,
+          _at(d_x), _at(d_weight), dwt, _at(d_bias), 1 if accumulate else 0, _at(ws), nb)
+    if stream is not None:
+        _used_on(stream, d_x, d_weight, d_bias, ws)
+    return d_x, d_weight, d_bias
 
 
 def loaded_library_path() -> str:
