@@ -22,7 +22,8 @@ ARCH = os.environ.get("RFT_OFFLOAD_ARCH", "gfx950")
 
 SOURCES = ["rft_abi.hip", "k_tokens.hip", "k_adv_loss.hip", "k_gemm_mfma.hip", "k_gemm_f32.hip",
            "k_layout.hip", "k_logits.hip", "k_step.hip", "k_pref.hip", "k_router.hip", "k_adamw.hip",
-           "k_ortho.hip", "k_expert.hip", "k_linear.hip", "k_linear_f32.hip"]
+           "k_ortho.hip", "k_expert.hip", "k_linear.hip",
+           "k_linear_few.hip", "k_linear_f32.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CFLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE, "-I", CSRC,

@@ -22,17 +22,9 @@ namespace rft {
 namespace lin {
 namespace {
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void* lds_ptr;
 
 enum { FWD = 0, DX = 1, DW = 2 };
 constexpr int BK = 64;
-
-// Raw buffer descriptor over 2^32 - 32 bytes from p; a lane that has nothing to read takes the
-// offset kNone, which lies past it and reads zeros.
-constexpr uint32_t kSpan = 0xffffffe0u, kNone = 0xfffffff0u;
 
 struct Args {
   Groups g;
@@ -47,43 +39,6 @@ struct Args {
   int slices;             // DW: of a group's rows; > 1: sums to part [slices, E, n, k]
   float* part;
 };
-
-__device__ __forceinline__ void barrier_lds() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-// s_waitcnt vmcnt(N), the other counters left alone.
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-  __builtin_amdgcn_s_waitcnt((N & 15) | 0x0F70 | ((N >> 4) << 14));
-}
-__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
-
-__device__ __forceinline__ uint64_t uniform(const void* p) {
-  const uint64_t a = (uint64_t)p;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
-  return ((uint64_t)hi << 32) | lo;
-}
-
-// 16 bytes per lane from base + v to LDS at dst + 16 lane.  Written out: in a kernel that reads
-// LDS transposed the compiler waits for every such load before each read.  It has no register
-// result, and the kernel's own waits cover it.
-__device__ __forceinline__ void load_lds(uint64_t base, char* dst, uint32_t v) {
-#ifdef __HIP_DEVICE_COMPILE__
-  const u32x4 w = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, kSpan, 0x00020000u};
-  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)dst);
-  // five wait states: scalar registers that a vector instruction has just written
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :
-               : "s"(at), "v"(v), "s"(w)
-               : "memory", "m0");
-#endif
-}
-__device__ __forceinline__ s16x4 read_tr(const char* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
-}
 
 // One operand of a tile of R rows (of its outer index), as a wave loads it: four 1 KiB pieces per
 // stage of 64 of the summed index.
@@ -150,14 +105,6 @@ __device__ __forceinline__ bf16x8 fragment(const char* s, int o, int ks) {
   const int granule = ((o >> 4) & 7) ^ ((r16 >> 2) | ((q4 & 1) << 2));
   const char* p = s + (o >> 7) * (BK * 256) + (ks * 32 + 8 * q4 + (r16 >> 2)) * 256 + granule * 32 + (r16 & 3) * 8;
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_tr(p), read_tr(p + 4 * 256), 0, 1, 2, 3, 4, 5, 6, 7));
-}
-
-__device__ __forceinline__ floatx4 load4(const uint16_t* p) {
-  const u16x4 h = *(const u16x4*)p;
-  return (floatx4){bf16_to_f32(h[0]), bf16_to_f32(h[1]), bf16_to_f32(h[2]), bf16_to_f32(h[3])};
-}
-__device__ __forceinline__ void store4(uint16_t* p, floatx4 v) {
-  *(u16x4*)p = (u16x4){f32_to_bf16(v[0]), f32_to_bf16(v[1]), f32_to_bf16(v[2]), f32_to_bf16(v[3])};
 }
 
 // Tiles of 256 x 256 (eight waves of 64 x 128, TP = 2) or 128 x 128 (four of 64 x 64, TP = 1).
@@ -301,9 +248,6 @@ __global__ void __launch_bounds__(kThreads<TP>, 2) k_lin(const Args g) {
     // element q of tile (i, j): row m0 + wm + 16 i + r16, column n0 + wn + 16 j + 4 q4 + q
     if constexpr (FORM == FWD) {
       const int64_t m = GLU ? n >> 1 : n;
-      const uint16_t* const bias = g.o.bias ? (const uint16_t*)g.o.bias + e * n : nullptr;
-      uint16_t *const y = (uint16_t*)g.o.y, *const z = (uint16_t*)g.o.z;
-      const uint16_t* const res = (const uint16_t*)g.o.residual;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int64_t r = rows.x + m0 + wm + i * 16 + r16;
@@ -312,20 +256,7 @@ __global__ void __launch_bounds__(kThreads<TP>, 2) k_lin(const Args g) {
         for (int j = 0; j < NJ; j += GLU ? 2 : 1) {
           const int64_t c = GLU ? (n0 + wn + j * 16) / 2 + q4 * 4 : n0 + wn + j * 16 + q4 * 4;
           if (c >= m) continue;
-          floatx4 v = acc[i][j], u = GLU ? acc[i][j + (GLU ? 1 : 0)] : v;
-          if (bias) {
-            v += load4(bias + c);
-            if (GLU) u += load4(bias + m + c);
-          }
-          if (z) {
-            store4(z + r * n + c, v);
-            if (GLU) store4(z + r * n + m + c, u);
-          }
-          floatx4 w;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) w[q] = GLU ? silu<true>(v[q]) * u[q] : act_of<true>(g.o.act, v[q]);
-          if (res) w += load4(res + r * m + c);
-          store4(y + r * m + c, w);
+          finish<GLU>(g.o, e, n, r, c, acc[i][j], acc[i][j + (GLU ? 1 : 0)]);
         }
       }
     } else if constexpr (FORM == DX) {
@@ -599,7 +530,7 @@ extern "C" {
 size_t rft_linear_workspace_bytes(const rft_groups* groups, int dtype, int64_t k, int64_t n,
                                   int32_t act) {
   if (check_groups("rft_linear_workspace_bytes", groups, dtype, k, n, act)) return 0;
-  return 0;
+  return dtype == RFT_BF16 ? linear_few_plan(*groups, k, n, act).ws_bytes : 0;
 }
 
 rft_status rft_linear(const rft_groups* groups, const void* x, const void* weight, int dtype,
@@ -618,6 +549,11 @@ rft_status rft_linear(const rft_groups* groups, const void* x, const void* weigh
   hipStream_t s = (hipStream_t)stream;
   if (dtype == RFT_F32) {
     RFT_HIP(linear_f32_fwd(g, (const float*)x, (const float*)weight, k, n, o, s), fn);
+    return RFT_OK;
+  }
+  const FewPlan few = linear_few_plan(*groups, k, n, act);
+  if (few.fits) {
+    RFT_HIP(linear_few(few, g, (const uint16_t*)x, (const uint16_t*)weight, k, n, o, (float*)ws, s), fn);
     return RFT_OK;
   }
   Args a = {};

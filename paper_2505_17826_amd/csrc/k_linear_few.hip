@@ -1,0 +1,249 @@
+// Linear layers on bf16 data with few rows per group: single tokens, decode steps.
+//
+// The weights are read once and each value multiplies a few rows, so HBM bounds it.  A block
+// owns 64 columns (RFT_ACT_SWIGLU: 32 of each half) of one group that has rows, and takes its
+// rows 16 MT at a time.  Stages of 128 of the summed index go straight to LDS, NS - 1 of them on
+// their way: what keeps HBM busy is bytes in flight, and those in LDS cost no registers.
+// (Weights straight to registers in the matrix instruction's layout, 64 bytes of 16 rows per
+// load, and the summed index dealt to the waves reached 2.8 TB/s.)  Where the blocks are few
+// the summed index is cut into slices, whose sums k_few_sum adds in order.
+#include <algorithm>
+#include <type_traits>
+
+#include "linear_device.h"
+
+namespace rft {
+namespace lin {
+namespace {
+
+// The i-th group that has rows; -1: none.  By whole waves.
+__device__ __forceinline__ int nth_group(const Groups& g, int i) {
+  if (!g.offsets) return i == 0 && g.rows > 0 ? 0 : -1;
+  const int lane = threadIdx.x & 63;
+  for (int e0 = 0; e0 < g.E; e0 += 256) {
+    uint64_t m[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int e = e0 + q * 64 + lane;
+      bool some = false;
+      if (e < g.E) {
+        const int2 r = rows_of(g, e);
+        some = r.y > r.x;
+      }
+      m[q] = __builtin_amdgcn_ballot_w64(some);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int c = __builtin_popcountll(m[q]);
+      if (i < c) {
+        const bool me = (m[q] >> lane & 1) && __builtin_popcountll(m[q] & ((1ull << lane) - 1)) == i;
+        return e0 + q * 64 + (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(me));
+      }
+      i -= c;
+    }
+  }
+  return -1;
+}
+
+struct Few {
+  Groups g;
+  const uint16_t *x, *w;
+  int64_t k, n;
+  Out o;
+  int slices;
+  float* part;  // [slices, rows, n], slices > 1
+};
+
+constexpr int BN = 64, BK = 128, NT = 256;
+
+// LDS rows of 256 bytes (BK values), 16-byte chunk c of row r at c ^ (r & 15): a fragment's reads
+// (16 rows, one chunk) touch every bank once.  A load fills four rows.
+__device__ __forceinline__ bf16x8 fragment(const char* s, int row, int chunk) {
+  return *(const bf16x8*)(s + row * 256 + ((chunk ^ (row & 15)) << 4));
+}
+
+template <bool GLU, int MT, int NS>
+__global__ void __launch_bounds__(NT) k_few(const Few f) {
+  constexpr int STAGE = (BN + MT * 16) * 256, L = 4 + MT;  // bytes; loads per wave
+  __shared__ __attribute__((aligned(16))) char lds[NS * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, q4 = lane >> 4;
+  const int e = nth_group(f.g, blockIdx.y);
+  if (e < 0) return;
+  const int2 rows = rows_of(f.g, e);
+  const int64_t half = f.n >> 1, m = GLU ? half : f.n, c0 = (int64_t)blockIdx.x * (GLU ? BN / 2 : BN);
+  // this block's share of the summed index
+  const int all = (int)((f.k + BK - 1) / BK);
+  const int s0 = (int)((int64_t)all * blockIdx.z / f.slices), s1 = (int)((int64_t)all * (blockIdx.z + 1) / f.slices);
+  const int nk = s1 - s0;
+  // wave w loads columns 16 w .. of the tile: GLU: the gate's and the other half's 16 in turn
+  const int64_t col = GLU ? c0 + (wave >> 1) * 16 : c0 + wave * 16;
+  const uint64_t wbase = uniform(f.w + (e * f.n + (GLU && (wave & 1) ? half : 0) + col) * f.k + (int64_t)s0 * BK);
+  uint32_t woff[4];
+  int wk[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 4 + q4;
+    wk[i] = (r16 ^ r) * 8;
+    woff[i] = col + r < m ? (uint32_t)((r * f.k + wk[i]) * 2) : kNone;
+  }
+  const int xk = (r16 ^ (wave * 4 + q4)) * 8;
+  const int K = (int)f.k - s0 * BK;
+  for (int r0 = rows.x; r0 < rows.y; r0 += MT * 16) {
+    const uint64_t xbase = uniform((f.g.source ? f.x : f.x + r0 * f.k) + (int64_t)s0 * BK);
+    uint32_t xoff[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int r = r0 + i * 16 + wave * 4 + q4;
+      const int64_t s = r >= rows.y ? -1 : f.g.source ? source_of(f.g, r) : r - r0;
+      xoff[i] = s < 0 ? kNone : (uint32_t)((s * f.k + xk) * 2);
+    }
+    auto load = [&](int t) {
+      char* const d = lds + (t % NS) * STAGE;
+      const int left = K - t * BK;
+      const uint64_t step = (uint64_t)t * (BK * 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        load_lds(wbase + step, d + wave * 4096 + i * 1024, wk[i] < left ? woff[i] : kNone);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+        load_lds(xbase + step, d + BN * 256 + i * 4096 + wave * 1024, xk < left ? xoff[i] : kNone);
+    };
+    floatx4 acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = (floatx4){0.f, 0.f, 0.f, 0.f};
+    wait_vm<0>();
+#pragma unroll
+    for (int t = 0; t < NS - 1; ++t)
+      if (t < nk) load(t);
+    for (int t = 0; t < nk; ++t) {
+      // this wave's loads of stage t have landed and its reads of stage t - 1 are done; then
+      // every wave's, and stage t - 1 can take stage t + NS - 1
+      const int ahead = min(nk - 1 - t, NS - 2);
+      if (ahead >= 2)
+        wait_vm<2 * L>();
+      else if (ahead == 1)
+        wait_vm<L>();
+      else
+        wait_vm<0>();
+      wait_lds();
+      barrier_lds();
+      if (t + NS - 1 < nk) load(t + NS - 1);
+      const char* const st = lds + (t % NS) * STAGE;
+#pragma unroll
+      for (int ks = 0; ks < BK / 32; ++ks) {
+        const bf16x8 w = fragment(st, wave * 16 + r16, ks * 4 + q4);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              w, fragment(st + BN * 256, i * 16 + r16, ks * 4 + q4), acc[i], 0, 0, 0);
+      }
+    }
+    wait_lds();
+    barrier_lds();  // the stages are free
+    // element q of tile i: row r0 + 16 i + r16, column col + 4 q4 + q
+    if (f.slices > 1) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int64_t r = r0 + i * 16 + r16, c = col + q4 * 4;
+        if (r < rows.y && c < m)
+          *(floatx4*)(f.part + ((int64_t)blockIdx.z * f.g.rows + r) * f.n + (GLU && (wave & 1) ? half : 0) + c) = acc[i];
+      }
+      continue;
+    }
+    if constexpr (GLU) {  // the other half's sums to the wave that has the gate's
+      floatx4* const other = (floatx4*)lds + (wave >> 1) * (MT * 64);
+      if (wave & 1) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) other[i * 64 + lane] = acc[i];
+      }
+      __syncthreads();
+      if (!(wave & 1)) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int64_t r = r0 + i * 16 + r16, c = col + q4 * 4;
+          if (r < rows.y && c < m) finish<true>(f.o, e, f.n, r, c, acc[i], other[i * 64 + lane]);
+        }
+      }
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int64_t r = r0 + i * 16 + r16, c = col + q4 * 4;
+        if (r < rows.y && c < m) finish<false>(f.o, e, f.n, r, c, acc[i], acc[i]);
+      }
+    }
+  }
+}
+
+// The slices' sums, in order, and the epilogue: four columns per thread.
+template <bool GLU>
+__global__ void __launch_bounds__(256) k_few_sum(const Few f) {
+  const int64_t m = GLU ? f.n >> 1 : f.n, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, r = blockIdx.y;
+  if (c >= m) return;
+  // the row's group: the last whose rows begin at or before it
+  int e = 0;
+  if (f.g.offsets) {
+    int hi = f.g.E;
+    while (hi - e > 1) {
+      const int mid = (e + hi) / 2;
+      if (f.g.offsets[mid] <= r) e = mid; else hi = mid;
+    }
+    const int2 rows = rows_of(f.g, e);
+    if (r < rows.x || r >= rows.y) return;
+  }
+  floatx4 v = {0.f, 0.f, 0.f, 0.f}, u = v;
+  for (int s = 0; s < f.slices; ++s) {
+    const float* const p = f.part + ((int64_t)s * f.g.rows + r) * f.n + c;
+    v += *(const floatx4*)p;
+    if (GLU) u += *(const floatx4*)(p + m);
+  }
+  finish<GLU>(f.o, e, f.n, r, c, v, u);
+}
+
+}  // namespace
+
+FewPlan linear_few_plan(const rft_groups& g, int64_t k, int64_t n, int act) {
+  FewPlan p = {};
+  const int64_t average = (g.rows + g.n_groups - 1) / g.n_groups;
+  p.fits = average <= 64 && g.rows <= 65535;
+  p.tiles = g.rows <= 16 || average <= 8 ? 1 : average <= 32 ? 2 : 4;
+  const int64_t blocks = (n + BN - 1) / BN * std::min<int64_t>(g.n_groups, g.rows);
+  p.slices = 1;
+  if (blocks > 0 && blocks < 128)
+    p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({512 / blocks, (k + BK - 1) / BK / 4, 16}));
+  p.ws_bytes = p.fits && p.slices > 1 ? (size_t)p.slices * g.rows * n * 4 : 0;
+  return p;
+}
+
+hipError_t linear_few(const FewPlan& p, const Groups& g, const uint16_t* x, const uint16_t* w,
+                      int64_t k, int64_t n, const Out& o, float* ws, hipStream_t s) {
+  const Few f = {g, x, w, k, n, o, p.slices, ws};
+  const bool glu = o.act == RFT_ACT_SWIGLU;
+  const dim3 grid((unsigned)((n + BN - 1) / BN), (unsigned)std::min(g.E, g.rows), (unsigned)p.slices);
+  auto go = [&](auto G, auto M, auto S) {
+    k_few<decltype(G)::value, decltype(M)::value, decltype(S)::value><<<grid, NT, 0, s>>>(f);
+  };
+  auto by_rows = [&](auto G) {
+    using std::integral_constant;
+    if (p.tiles == 1)
+      go(G, integral_constant<int, 1>{}, integral_constant<int, 3>{});
+    else if (p.tiles == 2)
+      go(G, integral_constant<int, 2>{}, integral_constant<int, 3>{});
+    else
+      go(G, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  };
+  glu ? by_rows(std::true_type{}) : by_rows(std::false_type{});
+  if (p.slices > 1) {
+    const int64_t m = glu ? n / 2 : n;
+    const dim3 sums((unsigned)((m / 4 + 255) / 256), (unsigned)g.rows);
+    if (glu)
+      k_few_sum<true><<<sums, 256, 0, s>>>(f);
+    else
+      k_few_sum<false><<<sums, 256, 0, s>>>(f);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace lin
+}  // namespace rft

@@ -93,6 +93,52 @@ __device__ __forceinline__ void tile_at(int t, int tm, int tn, int& i, int& j) {
   i = s * kStrip + r - j * h;
 }
 
+// --------------------------------------------------------- loads to LDS --
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+// Raw buffer descriptor over 2^32 - 32 bytes from p; a lane that has nothing to read takes the
+// offset kNone, which lies past it and reads zeros.
+constexpr uint32_t kSpan = 0xffffffe0u, kNone = 0xfffffff0u;
+
+__device__ __forceinline__ void barrier_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// s_waitcnt vmcnt(N), the other counters left alone.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | 0x0F70 | ((N >> 4) << 14));
+}
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+
+__device__ __forceinline__ uint64_t uniform(const void* p) {
+  const uint64_t a = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+  return ((uint64_t)hi << 32) | lo;
+}
+
+// 16 bytes per lane from base + v to LDS at dst + 16 lane.  Written out: in a kernel that reads
+// LDS transposed the compiler waits for every such load before each read.  It has no register
+// result, and the kernel's own waits cover it.
+__device__ __forceinline__ void load_lds(uint64_t base, char* dst, uint32_t v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  const u32x4 w = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, kSpan, 0x00020000u};
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)dst);
+  // five wait states: scalar registers that a vector instruction has just written
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :
+               : "s"(at), "v"(v), "s"(w)
+               : "memory", "m0");
+#endif
+}
+__device__ __forceinline__ s16x4 read_tr(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+}
+
 // ------------------------------------------------------------ activations --
 // Sigmoid.  FAST (bf16 data): exp2 of the rounded -x log2 e and a reciprocal, each good to
 // about 2^-22 where the value matters, against the 2^-9 of rounding the result.
@@ -142,6 +188,38 @@ struct Out {
   int act;
 };
 
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ floatx4 load4(const uint16_t* p) {
+  const u16x4 h = *(const u16x4*)p;
+  return (floatx4){bf16_to_f32(h[0]), bf16_to_f32(h[1]), bf16_to_f32(h[2]), bf16_to_f32(h[3])};
+}
+__device__ __forceinline__ void store4(uint16_t* p, floatx4 v) {
+  *(u16x4*)p = (u16x4){f32_to_bf16(v[0]), f32_to_bf16(v[1]), f32_to_bf16(v[2]), f32_to_bf16(v[3])};
+}
+
+// A forward's epilogue on bf16 data: columns [c, c + 4) of row r of group e from the product's v
+// (GLU: of the gate; u: of the other half).
+template <bool GLU>
+__device__ __forceinline__ void finish(const Out& o, int e, int64_t n, int64_t r, int64_t c, floatx4 v,
+                                       floatx4 u) {
+  const int64_t m = GLU ? n >> 1 : n;
+  if (o.bias) {
+    const uint16_t* const bias = (const uint16_t*)o.bias + e * n;
+    v += load4(bias + c);
+    if (GLU) u += load4(bias + m + c);
+  }
+  if (o.z) {
+    uint16_t* const z = (uint16_t*)o.z + r * n;
+    store4(z + c, v);
+    if (GLU) store4(z + m + c, u);
+  }
+  floatx4 w;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) w[q] = GLU ? silu<true>(v[q]) * u[q] : act_of<true>(o.act, v[q]);
+  if (o.residual) w += load4((const uint16_t*)o.residual + r * m + c);
+  store4((uint16_t*)o.y + r * m + c, w);
+}
+
 // dz in the workspace, and gradients of the bias (k_linear.hip).
 struct Dz {
   const void *dy, *z;
@@ -150,6 +228,17 @@ struct Dz {
   int act, accumulate;
   int64_t n;
 };
+
+// Few rows per group, bf16 (k_linear_few.hip).
+struct FewPlan {
+  bool fits;
+  int tiles;   // of 16 rows a block takes at a time
+  int slices;  // of the summed index; > 1: their sums in a workspace of ws_bytes
+  size_t ws_bytes;
+};
+FewPlan linear_few_plan(const rft_groups& g, int64_t k, int64_t n, int act);
+hipError_t linear_few(const FewPlan& p, const Groups& g, const uint16_t* x, const uint16_t* w,
+                      int64_t k, int64_t n, const Out& o, float* ws, hipStream_t s);
 
 // Entry points of the fp32 kernels (k_linear_f32.hip).
 hipError_t linear_f32_fwd(const Groups& g, const float* x, const float* w, int64_t k, int64_t n,
