@@ -36,7 +36,10 @@ CFLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE,
 # cross-lane moves; without NaN semantics the compiler drops the quieting of
 # each operand before every max (the hardware max still returns the non-NaN
 # operand, and exp/add still propagate a NaN into the sums).
-SOURCE_FLAGS = {"k_gemm_mfma.hip": ["-fno-honor-nans"]}
+# The products of k_linear's main loop are unrolled whole (accumulators are registers): more
+# than the compiler's default limit for a loop that asks for it.
+SOURCE_FLAGS = {"k_gemm_mfma.hip": ["-fno-honor-nans"],
+                "k_linear.hip": ["-mllvm", "-pragma-unroll-threshold=200000"]}
 
 
 def _compile(src, verbose=False, extra=()):

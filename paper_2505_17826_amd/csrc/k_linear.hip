@@ -23,8 +23,8 @@ namespace lin {
 namespace {
 
 
-enum { FWD = 0, DX = 1, DW = 2 };
-constexpr int BK = 64;
+enum { FWD = 0, DX = 1, DW = 2, DWS = 3 };  // DWS: DW with a source
+constexpr int BK = 64, NT = 256;
 
 struct Args {
   Groups g;
@@ -38,34 +38,38 @@ struct Args {
   int dw_bf16, accumulate;
   int slices;             // DW: of a group's rows; > 1: sums to part [slices, E, n, k]
   float* part;
+  const uint32_t* from;   // DW with a source: byte offsets of the rows of x (k_from)
 };
 
-// One operand of a tile of R rows (of its outer index), as a wave loads it: four 1 KiB pieces per
-// stage of 64 of the summed index.
+// One operand of a tile (its outer index), as a wave loads it: P pieces of 1 KiB per stage of 64
+// of the summed index.
 //  rows  (summed index contiguous): LDS rows of 128 bytes, 16-byte chunk c of row r at
 //        c ^ ((r >> 1) & 7); a piece is eight rows.  A fragment's ds_read_b128 (16 rows, one
-//        chunk) then touches every bank once per 16 lanes.
+//        chunk) then touches every bank once per 16 lanes.  (Stages of 32, rows of 64 bytes: half
+//        cache lines per request, and the products wait for L2: 1060 TFLOP/s at 16384 x 4096 x
+//        8192.)
 //  cols  (summed index is the row): blocks of 64 rows x 128 columns, rows of 256 bytes, the
 //        32-byte granule q of row r at q ^ ((r & 3) | (r >> 3 & 1) << 2); a piece is four rows.
 //        A transposed read takes 32 bytes of rows 8 g .. 8 g + 3 for two (g, g + 1) of the four
 //        lane groups at a time: eight granules, every bank once.
-template <bool COLS>
+template <bool COLS, int P>
 struct Operand {
-  uint64_t base;      // of the stage to load next
-  uint32_t off[4];    // of the wave's pieces; kNone: zeros
-  int64_t step;       // bytes per stage
-  int at[2];          // rows: first element of the chunk for even and odd pieces; cols: row in the stage of piece 0
+  uint64_t base;    // of the stage to load next
+  uint64_t here;    // of the stage being loaded
+  uint32_t off[P];  // of the wave's pieces; kNone: zeros
+  uint32_t step;    // bytes per stage
+  int at[2];        // rows: first element of the lane's chunk in even and odd pieces; cols: its row
+                    // in the stage, piece 0
 
-  // rows: outer index o of piece row (0 .. R); row(o): its element offset, or -1.
-  // cols: column(c): element offset of 8 columns from c, or -1.
+  // rows: f(r) = element offset of row r of the tile, cols: of column c; -1: zeros.
   template <class F>
   __device__ __forceinline__ void start(const void* p, int64_t ld, F f) {
     const int lane = threadIdx.x & 63;
-    const int q0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 4;
+    const int q0 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * P;
     base = uniform(p);
-    step = COLS ? ld * (BK * 2) : BK * 2;
+    step = (uint32_t)(COLS ? ld * (BK * 2) : BK * 2);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < P; ++i) {
       const int q = q0 + i;
       if (COLS) {
         const int row = (q & 15) * 4 + (lane >> 4);
@@ -81,46 +85,61 @@ struct Operand {
       }
     }
   }
-  // left: of the summed index from this stage on
-  __device__ __forceinline__ void load(char* dst, int left) {
-    char* const d = dst + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 4096;
+  // What lies past the end of the summed index, of which `left` (< BK) is left from this stage on,
+  // is zeros, in this stage and all after it.
+  __device__ __forceinline__ void end(int left) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t v = off[i];
-      if (left < BK && (COLS ? at[0] + 4 * i : at[i & 1]) >= left) v = kNone;
-      load_lds(base, d + i * 1024, v);
+    for (int i = 0; i < P; ++i)
+      if ((COLS ? at[0] + 4 * i : at[i & 1]) >= left) off[i] = kNone;
+  }
+  // Piece i of a stage to dst, where the wave's pieces lie.
+  template <bool NOPS>
+  __device__ __forceinline__ void load(int i, uint32_t dst, uint32_t v) {
+    if (i == 0) {  // (into scalar registers: the compiler may hold it in others)
+      here = uniform((const void*)base);
+      base += step;
+      load_lds<true>(here, dst, v);
+    } else {
+      load_lds<NOPS>(here, dst + i * 1024, v);
     }
-    base += step;
   }
 };
 
-// The fragment of 16 of the outer index from o on, of summed indices 32 ks + 8 (lane / 16) ..
+// Half h (of 1 or 2) of the fragment of 16 of the outer index from o on, summed indices
+// 32 ks + 8 (lane / 16) ..
 template <bool COLS>
-__device__ __forceinline__ bf16x8 fragment(const char* s, int o, int ks) {
+__device__ __forceinline__ void read_fragment(const char* s, int o, int ks, int h, bf16x8& f,
+                                              s16x4 (&half)[2]) {
   const int r16 = threadIdx.x & 15, q4 = (threadIdx.x & 63) >> 4;
   if (!COLS) {
     const int row = o + r16;
-    return *(const bf16x8*)(s + row * 128 + (((ks * 4 + q4) ^ ((row >> 1) & 7)) << 4));
+    f = *(const bf16x8*)(s + row * 128 + (((ks * 4 + q4) ^ ((row >> 1) & 7)) << 4));
+  } else {
+    const int granule = ((o >> 4) & 7) ^ ((r16 >> 2) | ((q4 & 1) << 2));
+    half[h] = read_tr(s + (o >> 7) * (BK * 256) + (ks * 32 + 8 * q4 + 4 * h + (r16 >> 2)) * 256 +
+                      granule * 32 + (r16 & 3) * 8);
   }
-  const int granule = ((o >> 4) & 7) ^ ((r16 >> 2) | ((q4 & 1) << 2));
-  const char* p = s + (o >> 7) * (BK * 256) + (ks * 32 + 8 * q4 + (r16 >> 2)) * 256 + granule * 32 + (r16 & 3) * 8;
-  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(read_tr(p), read_tr(p + 4 * 256), 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Tiles of 256 x 256 (eight waves of 64 x 128, TP = 2) or 128 x 128 (four of 64 x 64, TP = 1).
-template <int TP> constexpr int kThreads = TP == 2 ? 512 : 256;
-
-template <int FORM, int TP, bool GLU>
-__global__ void __launch_bounds__(kThreads<TP>, 2) k_lin(const Args g) {
-  constexpr int NT = kThreads<TP>, BM = 128 * TP, BN = 128 * TP;
-  constexpr int NJ = 4 * TP;                       // 16-column tiles of a wave
+// Tiles of 32 MI x 32 NJ, four waves of 16 MI x 16 NJ, two stages of 64 of the summed index in
+// LDS, each multiplied in two halves of 32.  The fragments of a half are read to registers between
+// the products of the half before it.
+template <int FORM_, int MI, int NJ, int ACT>
+__global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
+  constexpr bool GLU = ACT == RFT_ACT_SWIGLU, SRC = FORM_ == DWS;
+  constexpr int FORM = SRC ? DW : FORM_;
+  constexpr int BM = 32 * MI, BN = 32 * NJ;
   constexpr bool AC = FORM == DW, BC = FORM != FWD;  // operands whose summed index is the row
-  constexpr int OPB = BM * BK * 2, STAGE = 2 * OPB;
+  constexpr int PA = MI, PB = NJ, L = PA + PB;  // loads per wave and stage
+  constexpr int OPA = BM * BK * 2, STAGE = (BM + BN) * BK * 2;
+  constexpr int RA = (AC ? 2 : 1) * MI, RD = RA + (BC ? 2 : 1) * NJ;  // reads per stage
+  constexpr int PD = MI * NJ;                                         // products
   __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
-  __shared__ int tab[kMaxGroups + 1], sh[NT / 64];
+  __shared__ int tab[FORM == DW ? 1 : kMaxGroups + 1], sh[NT / 64];
+  __shared__ uint32_t ring[SRC ? NT / 64 : 1][4][BK];  // DW with a source: offsets of stages' rows
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = (wid >> 1) * 64, wn = (wid & 1) * (16 * NJ);
+  const int wm = (wid >> 1) * (16 * MI), wn = (wid & 1) * (16 * NJ);
   const int r16 = lane & 15, q4 = lane >> 4;
   const int64_t k = g.k, n = g.n;
   int items;
@@ -128,54 +147,68 @@ __global__ void __launch_bounds__(kThreads<TP>, 2) k_lin(const Args g) {
     items = g.most;
   } else {
     tile_table<NT, BM>(g.g, g.tn, g.most, tab, sh);
-    items = tab[g.g.E];
+    items = __builtin_amdgcn_readfirstlane(tab[g.g.E]);
   }
   // Blocks go round the eight XCDs, each with an L2 of its own: XCD x takes the x-th eighth of
   // the tiles.
   const int xcd = blockIdx.x & 7, per = (items + 7) / 8;
   const int last = min(items, (xcd + 1) * per);
-  for (int item = xcd * per + (blockIdx.x >> 3); item < last; item += gridDim.x >> 3) {
-    int e, ti, tj, slice = 0;
+
+  struct Tile {
+    int e, m0, n0, slice, y;  // group, first row and column of the tile, end of the group's rows
+    int64_t x;                // the group's first row
+  };
+  Operand<AC, PA> A;
+  Operand<BC, PB> B;
+  int K = 0, left = 0;  // of the summed index: all, and from the stage to load next on
+  const uint32_t places = lds_at(ring[wid]);
+  uint64_t from = 0;    // DW with a source: of the offsets to load next, and their place
+  int fs = 0;
+  // Offsets of the rows of one more stage; they are used a stage later.
+  auto load_from = [&]() {
+    load_lds4(from, places + fs * (BK * 4), lane * 4);
+    from += BK * 4;
+    fs = (fs + 1) & 3;
+  };
+  // The tile of an item and its operands; false: none (invalid offsets).
+  auto set = [&](int item, Tile& t) {
+    int ti, tj;
+    t.slice = 0;
     if constexpr (FORM == DW) {
       const int tm = (int)((n + BM - 1) / BM), each = tm * g.tn;
-      e = item / each;
-      tile_at(item - e * each, tm, g.tn, ti, tj);
-      slice = e % g.slices;
-      e /= g.slices;
+      t.e = item / each;
+      tile_at(item - t.e * each, tm, g.tn, ti, tj);
+      t.slice = t.e % g.slices;
+      t.e /= g.slices;
     } else {
-      e = group_of(tab, g.g.E, item);
+      t.e = group_of(tab, g.g.E, item);
     }
-    int2 rows = rows_of(g.g, e);
-    rows.x = __builtin_amdgcn_readfirstlane(rows.x);
-    rows.y = __builtin_amdgcn_readfirstlane(rows.y);
+    const int2 rows = rows_of(g.g, t.e);
+    t.x = __builtin_amdgcn_readfirstlane(rows.x);
+    t.y = __builtin_amdgcn_readfirstlane(rows.y);
     if constexpr (FORM != DW) {
-      const int tm = (rows.y - rows.x + BM - 1) / BM, t = item - tab[e];
-      if ((unsigned)t >= (unsigned)(tm * g.tn)) continue;
-      tile_at(t, tm, g.tn, ti, tj);
+      const int tm = (int)(t.y - t.x + BM - 1) / BM, i = __builtin_amdgcn_readfirstlane(item - tab[t.e]);
+      if ((unsigned)i >= (unsigned)(tm * g.tn)) return false;
+      tile_at(i, tm, g.tn, ti, tj);
     } else if (g.slices > 1) {
-      const int c = (rows.y - rows.x + BK - 1) / BK;  // in whole stages
-      const int64_t x0 = rows.x;
-      rows.x = (int)(x0 + (int64_t)c * slice / g.slices * BK);
-      rows.y = (int)min((int64_t)rows.y, x0 + (int64_t)c * (slice + 1) / g.slices * BK);
+      const int c = (int)((t.y - t.x + BK - 1) / BK);  // in whole stages
+      const int64_t x0 = t.x;
+      t.x = x0 + (int64_t)c * t.slice / g.slices * BK;
+      t.y = (int)min((int64_t)t.y, x0 + (int64_t)c * (t.slice + 1) / g.slices * BK);
     }
-    const int m0 = ti * BM, n0 = tj * BN;
-    const uint16_t* const we = (FORM == DW ? g.b : g.b + e * n * k);
-    Operand<AC> A;
-    Operand<BC> B;
-    int K;  // summed index
+    const int m0 = t.m0 = ti * BM, n0 = t.n0 = tj * BN;
+    const int rest = (int)(t.y - t.x) - m0;  // FWD, DX: rows of the group from the tile on
+    const uint16_t* const we = FORM == DW ? g.b : g.b + t.e * n * k;
     if constexpr (FORM == FWD) {
       K = (int)k;
-      const int64_t f = n >> 1;
+      const int64_t f = n >> 1, r0 = t.x + m0;
       if (g.g.source)
         A.start(g.a, k, [&](int o) -> int64_t {
-          const int r = rows.x + m0 + o;
-          if (r >= rows.y) return -1;
-          const int64_t s = source_of(g.g, r);
+          const int64_t s = o < rest ? source_of(g.g, (int)r0 + o) : -1;
           return s < 0 ? -1 : s * k;
         });
       else
-        A.start(g.a + (int64_t)(rows.x + m0) * k, k,
-                [&](int o) -> int64_t { return rows.x + m0 + o < rows.y ? o * k : -1; });
+        A.start(g.a + r0 * k, k, [&](int o) -> int64_t { return o < rest ? o * k : -1; });
       if constexpr (GLU)  // 16 columns of the gate, then the same 16 of the other half
         B.start(we, k, [&](int o) -> int64_t {
           const int64_t c = (n0 >> 1) + (o >> 5) * 16 + (o & 15);
@@ -185,113 +218,238 @@ __global__ void __launch_bounds__(kThreads<TP>, 2) k_lin(const Args g) {
         B.start(we + n0 * k, k, [&](int o) -> int64_t { return n0 + o < n ? o * k : -1; });
     } else if constexpr (FORM == DX) {
       K = (int)n;
-      A.start(g.a + (int64_t)(rows.x + m0) * n, n,
-              [&](int o) -> int64_t { return rows.x + m0 + o < rows.y ? o * n : -1; });
+      A.start(g.a + (t.x + m0) * n, n, [&](int o) -> int64_t { return o < rest ? o * n : -1; });
       B.start(we + n0, k, [&](int c) -> int64_t { return n0 + c < k ? c : -1; });
     } else {
-      K = rows.y - rows.x;
-      A.start(g.a + rows.x * n + m0, n, [&](int c) -> int64_t { return m0 + c < n ? c : -1; });
-      B.start(g.g.source ? we + n0 : we + rows.x * k + n0, k,
-              [&](int c) -> int64_t { return n0 + c < k ? c : -1; });
-    }
-    int srow = rows.x;  // DW with a source: the stage's first row
-    auto load = [&](int st, int left) {
-      A.load(lds + st * STAGE, left);
-      if (FORM == DW && g.g.source) {
-        Operand<BC> S = B;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = srow + B.at[0] + 4 * i;
-          const int64_t s = r < rows.y ? source_of(g.g, r) : -1;
-          if (B.off[i] != kNone)
-            S.off[i] = s < 0 ? kNone : (uint32_t)((int64_t)B.off[i] + (s - B.at[0] - 4 * i) * k * 2);
-        }
-        S.load(lds + st * STAGE + OPB, left);
-        srow += BK;
-      } else {
-        B.load(lds + st * STAGE + OPB, left);
+      K = (int)(t.y - t.x);
+      A.start(g.a + t.x * n + m0, n, [&](int c) -> int64_t { return m0 + c < n ? c : -1; });
+      B.start(SRC ? we + n0 : we + t.x * k + n0, k, [&](int c) -> int64_t { return n0 + c < k ? c : -1; });
+      if constexpr (SRC) {
+        B.step = 0;
+        from = uniform(g.from + t.x);
+        load_from();
+        load_from();
+        load_from();
+        wait_vm<0>();
+        fs = 0;
       }
-    };
-    floatx4 acc[4][NJ];
+    }
+    left = K;
+    return true;
+  };
+  const uint32_t place = lds_at(lds) + wid * (PA * 1024);  // of the wave's pieces of A
+  const uint32_t placeB = OPA + wid * ((PB - PA) * 1024);  // and of B, from there
+  // The x-th load of the stage to load next, to the stage at byte `st` of LDS.
+  auto load_one = [&](auto nops, uint32_t st, int x) {
+    constexpr bool NOPS = decltype(nops)::value;
+    if (x == 0 && left < BK) {
+      A.end(left);
+      B.end(left);
+    }
+    if (x < PA) {
+      A.template load<NOPS>(x, place + st, A.off[x]);
+    } else {
+      const int i = x - PA;
+      uint32_t v = B.off[i];
+      if constexpr (SRC) {  // off has the place of the stage's row in consecutive rows
+        const int r = B.at[0] + 4 * i;
+        const uint32_t row = ring[wid][fs][r];
+        v = v != kNone && row != kNone ? v - (uint32_t)r * (uint32_t)(k * 2) + row : kNone;
+      }
+      B.template load<NOPS>(i, place + placeB + st, v);
+    }
+    if (x == L - 1) {
+      left -= BK;
+      if constexpr (SRC) {
+        fs = (fs + 3) & 3;
+        load_from();
+        fs = (fs + 1) & 3;
+      }
+    }
+  };
+
+  floatx4 acc[MI][NJ];
+  bf16x8 fa[2][MI], fb[2][NJ];
+  s16x4 ha[2][MI][2], hb[2][NJ][2];
+  // The x-th read of the fragments of half s of a stage, the q-th product.
+  auto read_one = [&](int s, const char* st, int x) {
+    if (x < RA) {
+      const int i = AC ? x / 2 : x;
+      read_fragment<AC>(st, wm + i * 16, s, x & 1, fa[s][i], ha[s][i]);
+    } else {
+      const int y = x - RA, j = BC ? y / 2 : y;
+      read_fragment<BC>(st + OPA, wn + j * 16, s, y & 1, fb[s][j], hb[s][j]);
+    }
+  };
+  auto whole = [](const s16x4 (&h)[2]) {
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto multiply_one = [&](int s, int q) {
+    const int i = q / NJ, j = q % NJ;
+    const bf16x8 a = AC ? whole(ha[s][i]) : fa[s][i], b = BC ? whole(hb[s][j]) : fb[s][j];
+    // b first: the order that gives a lane four columns of a row
+    if constexpr (MI < 8) {
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, acc[i][j], 0, 0, 0);
+    } else {
+#ifdef __HIP_DEVICE_COMPILE__
+      // Written out: the sums fill the accumulation registers, and left to itself the compiler
+      // moves them about (290 moves per stage).  It does not know the wait states around an
+      // instruction that it did not choose; see settle().
+      asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[i][j]) : "v"(b), "v"(a));
+#endif
+    }
+  };
+
+  // Wait states between the products and what else writes or reads the sums: 24, of which a
+  // result needs 18.  Products go out 16 cycles apart, so of the first or last ones of a loop
+  // four are tied to it; the others are further away by themselves.
+  auto settle = [&](floatx4& a, floatx4& b, floatx4& c, floatx4& d) {
+#ifdef __HIP_DEVICE_COMPILE__
+    if constexpr (MI == 8)
+      asm volatile("s_nop 15\n\ts_nop 7" : "+a"(a), "+a"(b), "+a"(c), "+a"(d) : : "memory");
+#endif
+  };
+
+  Tile t;
+  int item = xcd * per + (blockIdx.x >> 3);
+  const int stride = gridDim.x >> 3;
+  auto next = [&]() {  // sets the next tile and issues its first stages
+    for (; item < last; item += stride) {
+      if (!set(item, t)) continue;
+      item += stride;
+      // (what the operands' set-up read has landed)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int x = 0; x < L; ++x) load_one(std::true_type{}, p * STAGE, x);
+      return true;
+    }
+    return false;
+  };
+  while (next()) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
     const int nk = (K + BK - 1) / BK;
-    wait_vm<0>();
-    if (nk > 0) load(0, K);
-    if (nk > 1) load(1, K - BK);
+    wait_vm<L + (SRC ? 1 : 0)>();  // stage 0
+    barrier_lds();
+#pragma unroll
+    for (int x = 0; x < RD; ++x) read_one(0, lds, x);
+    // A stage is Q products, the second half of it on other fragments:
+    //   [0, R1)       the reads of the second half's fragments
+    //   F             every wave has them: the stage's place is free
+    //   [F, F + SP)   the loads of the stage after the next one, to this place, spread out: the
+    //                 path from L2 is busy half of the time
+    //   W             the next stage has landed: the loads before those of this stage are done
+    //   [W, Q)        the reads of its first half's fragments
+    constexpr int Q = 2 * PD, R1 = Q / 4, F = R1 + Q / 16, SP = Q * 9 / 16, W = Q * 5 / 8;
+    constexpr int R2 = Q / 4;
+    constexpr int UNDER = ((W - F) * L + SP - 1) / SP;  // loads of this stage issued before W
+    settle(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);
     for (int kt = 0; kt < nk; ++kt) {
-      if (kt + 1 < nk)
-        wait_vm<8>();
-      else
-        wait_vm<0>();
-      barrier_lds();
-      const char* const sa = lds + (kt & 1) * STAGE;
+      char* const cur = lds + (kt & 1) * STAGE;
+      const char* const nxt = lds + ((kt & 1) ^ 1) * STAGE;
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        bf16x8 fa[4], fb[NJ];
+      for (int q = 0; q < Q; ++q) {
+        if (q == F) {
+          wait_lds();
+          barrier_lds();
+        }
+        if (q == W) {
+          wait_vm<UNDER>();
+          barrier_lds();
+        }
+        multiply_one(q / PD, q % PD);
+        if (q < R1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) fa[i] = fragment<AC>(sa, wm + i * 16, ks);
+          for (int x = q * RD / R1; x < (q + 1) * RD / R1; ++x) read_one(1, cur, x);
+        }
+        if (q >= F && q < F + SP) {
+          // load x goes out after product F + x SP / L
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) fb[j] = fragment<BC>(sa + OPB, wn + j * 16, ks);
+          for (int x = ((q - F) * L + SP - 1) / SP; x < ((q - F + 1) * L + SP - 1) / SP; ++x)
+            load_one(std::false_type{}, (kt & 1) * STAGE, x);
+        }
+        if (q >= W && q < W + R2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)  // in the order that gives a lane four columns of a row
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+          for (int x = (q - W) * RD / R2; x < (q - W + 1) * RD / R2; ++x) read_one(0, nxt, x);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-      wait_lds();
-      barrier_lds();
-      if (kt + 2 < nk) load(kt & 1, K - (kt + 2) * BK);
     }
-    // element q of tile (i, j): row m0 + wm + 16 i + r16, column n0 + wn + 16 j + 4 q4 + q
-    if constexpr (FORM == FWD) {
-      const int64_t m = GLU ? n >> 1 : n;
+    settle(acc[MI - 1][NJ - 4], acc[MI - 1][NJ - 3], acc[MI - 1][NJ - 2], acc[MI - 1][NJ - 1]);
+    wait_vm<0>();
+    wait_lds();
+    barrier_lds();  // no load is under way, the stages are free
+    // Element q of tile (i, j) is row 16 i + r16, column 16 j + 4 q4 + q of the wave's part.  64 rows
+    // at a time go through LDS (16-byte chunk c of row r at c ^ (r & 15)), so that a lane has eight
+    // columns of a row and a row is written in whole cache lines.
+    float* const mine = (float*)(lds + wid * (STAGE / 2));
+    constexpr int CH = 4 * NJ;  // chunks per row
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t r = rows.x + m0 + wm + i * 16 + r16;
-        if (r >= rows.y) continue;
+    for (int h = 0; h < MI / 4; ++h) {
 #pragma unroll
-        for (int j = 0; j < NJ; j += GLU ? 2 : 1) {
-          const int64_t c = GLU ? (n0 + wn + j * 16) / 2 + q4 * 4 : n0 + wn + j * 16 + q4 * 4;
-          if (c >= m) continue;
-          finish<GLU>(g.o, e, n, r, c, acc[i][j], acc[i][j + (GLU ? 1 : 0)]);
-        }
-      }
-    } else if constexpr (FORM == DX) {
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t r = rows.x + m0 + wm + i * 16 + r16;
-        if (r >= rows.y) continue;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const int64_t c = n0 + wn + j * 16 + q4 * 4;
-          if (c < k) store4(g.dx + r * k + c, acc[i][j]);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t r = m0 + wm + i * 16 + r16;
-        if (r >= n) continue;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const int64_t c = n0 + wn + j * 16 + q4 * 4;
-          if (c >= k) continue;
-          const int64_t at = (e * n + r) * k + c;
+        for (int j = 0; j < NJ; ++j)
+          *(floatx4*)(mine + ((i * 16 + r16) * CH + ((j * 4 + q4) ^ r16)) * 4) = acc[h * 4 + i][j];
+      wait_lds();
+      __builtin_amdgcn_wave_barrier();
+      constexpr int OC = GLU ? 8 * NJ : 16 * NJ, LR = OC / 8;  // columns out; lanes per row
+      const int oc = (lane % LR) * 8;
+      const int64_t c = (GLU ? (t.n0 + wn) / 2 : t.n0 + wn) + oc;
+#pragma unroll 1
+      for (int row = lane / LR; row < 64; row += 64 / LR) {
+        const int64_t o = t.m0 + wm + h * 64 + row;
+        auto get = [&](int col) {
+          return *(const floatx4*)(mine + (row * CH + ((col >> 2) ^ (row & 15))) * 4);
+        };
+        // GLU: 16 columns of the gate, 16 of the other half in turn
+        const int v = GLU ? (oc >> 4) * 32 + (oc & 15) : oc;
+        const floatx4 v0 = get(v), v1 = get(v + 4);
+        if constexpr (FORM == FWD) {
+          if (t.x + o < t.y && c < (GLU ? n >> 1 : n)) {
+            floatx4 u0 = v0, u1 = v1;
+            if (GLU) {
+              u0 = get(v + 16);
+              u1 = get(v + 20);
+            }
+            finish8<ACT>(g.o, t.e, n, t.x + o, c, v0, v1, u0, u1);
+          }
+        } else if constexpr (FORM == DX) {
+          if (t.x + o < t.y && c < k) store8(g.dx + (t.x + o) * k + c, v0, v1);
+        } else if (o < n && c < k) {
+          const int64_t at = (t.e * n + o) * k + c;
           if (g.slices > 1) {
-            *(floatx4*)(g.part + (int64_t)slice * g.g.E * n * k + at) = acc[i][j];
+            floatx4* const p = (floatx4*)(g.part + (int64_t)t.slice * g.g.E * n * k + at);
+            p[0] = v0;
+            p[1] = v1;
           } else if (g.dw_bf16) {
-            store4((uint16_t*)g.dw + at, acc[i][j]);
+            store8((uint16_t*)g.dw + at, v0, v1);
           } else {
             floatx4* const p = (floatx4*)((float*)g.dw + at);
-            *p = g.accumulate ? *p + acc[i][j] : acc[i][j];
+            p[0] = g.accumulate ? p[0] + v0 : v0;
+            p[1] = g.accumulate ? p[1] + v1 : v1;
           }
         }
       }
+      wait_lds();
+      __builtin_amdgcn_wave_barrier();
     }
+    barrier_lds();  // the stages are free for the next tile
   }
+}
+
+// Byte offsets of the rows of x behind the groups' rows (kNone: zeros), and of kFromPad rows past
+// them, which the stages at the end read.  d_weight's product brings them to LDS a stage before
+// it loads the rows, so no load waits for another.
+constexpr int kFromPad = 8 * BK;
+__global__ void __launch_bounds__(256) k_from(const Groups g, int64_t k, uint32_t* from) {
+  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (r >= (int64_t)g.rows + kFromPad) return;
+  const int64_t s = r < g.rows ? source_of(g, (int)r) : -1;
+  from[r] = s < 0 ? kNone : (uint32_t)(s * k * 2);
 }
 
 // d_weight from the slices' sums, in order; four elements per thread (count % 4 == 0).
@@ -465,26 +623,27 @@ rft_status check_aligned(const char* fn, int dtype, std::initializer_list<const 
   return RFT_OK;
 }
 
-template <int FORM, int TP, bool GLU>
-hipError_t launch_lin(Args a, int64_t outer, int64_t across, hipStream_t s) {
-  // outer: FWD, DX: rows; DW: n
-  constexpr int B = 128 * TP;
-  a.tn = (int)ceil_div(across, B);
-  const int64_t tiles = FORM == DW ? a.g.E * a.slices * ceil_div(outer, B) * a.tn
-                                   : (outer / B + a.g.E) * a.tn;
+template <int FORM, int MI, int NJ, int ACT>
+hipError_t launch_lin(Args a, int64_t tiles, int64_t across, hipStream_t s) {
+  a.tn = (int)ceil_div(across, 32 * NJ);
   a.most = (int)tiles;
-  // a whole round of blocks (TP 2: one per CU, TP 1: two), a multiple of the XCDs
-  const int64_t round = TP == 2 ? 256 : 512;
+  // a whole round of blocks, a multiple of the XCDs
+  const int64_t round = MI == 8 ? 256 : 512;
   const unsigned grid = (unsigned)std::min<int64_t>(round, ceil_div(tiles, 8) * 8);
-  k_lin<FORM, TP, GLU><<<grid, kThreads<TP>, 0, s>>>(a);
+  k_lin<FORM, MI, NJ, ACT><<<grid, NT, 0, s>>>(a);
   return hipGetLastError();
 }
 
-template <int FORM, bool GLU>
+// outer: FWD, DX: rows; DW: n
+template <int FORM, int ACT>
 hipError_t launch_tiles(const Args& a, int64_t outer, int64_t across, hipStream_t s) {
-  const int64_t big = FORM == DW ? a.g.E * a.slices * ceil_div(outer, 256) * ceil_div(across, 256)
-                                 : (outer / 256 + a.g.E) * ceil_div(across, 256);
-  return big >= 256 ? launch_lin<FORM, 2, GLU>(a, outer, across, s) : launch_lin<FORM, 1, GLU>(a, outer, across, s);
+  auto tiles = [&](int64_t bm, int64_t bn) {
+    return FORM >= DW ? a.g.E * a.slices * ceil_div(outer, bm) * ceil_div(across, bn)
+                      : (outer / bm + a.g.E) * ceil_div(across, bn);
+  };
+  if (tiles(256, 256) >= 256)
+    return launch_lin<FORM, 8, 8, ACT>(a, tiles(256, 256), across, s);
+  return launch_lin<FORM, 4, 4, ACT>(a, tiles(128, 128), across, s);
 }
 
 // Slices of a group's rows for d_weight: where its tiles leave CUs idle and the rows are many.
@@ -503,6 +662,7 @@ struct BwdWs {
   void* dz;
   double* bias;
   float* dw;
+  uint32_t* from;
   size_t bytes;
 };
 BwdWs carve_bwd(void* base, const rft_groups& g, int dtype, int64_t k, int64_t n, int act) {
@@ -514,6 +674,7 @@ BwdWs carve_bwd(void* base, const rft_groups& g, int dtype, int64_t k, int64_t n
   w.bias = c.take<double>((size_t)std::max(dz_slices(g, m, 1), dz_slices(g, m, 8)) * g.n_groups * n);
   const int s = dw_slices(g, k, n);
   w.dw = s > 1 ? c.take<float>((size_t)s * g.n_groups * n * k) : nullptr;
+  w.from = dtype == RFT_BF16 && g.source ? c.take<uint32_t>((size_t)g.rows + kFromPad) : nullptr;
   w.bytes = c.bytes();
   return w;
 }
@@ -545,15 +706,15 @@ rft_status rft_linear(const rft_groups* groups, const void* x, const void* weigh
   if ((st = check_aligned(fn, dtype, {x, weight, bias, residual, y, z}))) return st;
   if ((st = check_ws(fn, ws, ws_bytes, rft_linear_workspace_bytes(groups, dtype, k, n, act)))) return st;
   const Groups g = groups_of(*groups);
-  const Out o = {bias, residual, y, z, act};
+  const Out o = {bias, residual, y, z};
   hipStream_t s = (hipStream_t)stream;
   if (dtype == RFT_F32) {
-    RFT_HIP(linear_f32_fwd(g, (const float*)x, (const float*)weight, k, n, o, s), fn);
+    RFT_HIP(linear_f32_fwd(g, (const float*)x, (const float*)weight, k, n, act, o, s), fn);
     return RFT_OK;
   }
   const FewPlan few = linear_few_plan(*groups, k, n, act);
   if (few.fits) {
-    RFT_HIP(linear_few(few, g, (const uint16_t*)x, (const uint16_t*)weight, k, n, o, (float*)ws, s), fn);
+    RFT_HIP(linear_few(few, g, (const uint16_t*)x, (const uint16_t*)weight, k, n, act, o, (float*)ws, s), fn);
     return RFT_OK;
   }
   Args a = {};
@@ -563,8 +724,9 @@ rft_status rft_linear(const rft_groups* groups, const void* x, const void* weigh
   a.k = k;
   a.n = n;
   a.o = o;
-  RFT_HIP(act == RFT_ACT_SWIGLU ? (launch_tiles<FWD, true>(a, groups->rows, n, s))
-                                : (launch_tiles<FWD, false>(a, groups->rows, n, s)), fn);
+  hipError_t err = hipSuccess;
+  by_act(act, [&](auto A) { err = launch_tiles<FWD, decltype(A)::value>(a, groups->rows, n, s); });
+  RFT_HIP(err, fn);
   return RFT_OK;
 }
 
@@ -634,7 +796,7 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
   if (d_x && any) {
     a.b = (const uint16_t*)weight;
     a.dx = (uint16_t*)d_x;
-    RFT_HIP((launch_tiles<DX, false>(a, groups->rows, k, s)), fn);
+    RFT_HIP((launch_tiles<DX, RFT_ACT_NONE>(a, groups->rows, k, s)), fn);
   }
   if (d_weight) {
     a.b = (const uint16_t*)x;
@@ -643,7 +805,12 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
     a.accumulate = accumulate;
     a.slices = slices;
     a.part = w.dw;
-    RFT_HIP((launch_tiles<DW, false>(a, n, k, s)), fn);
+    if (g.source) {
+      a.from = w.from;
+      k_from<<<(unsigned)ceil_div(g.rows + kFromPad, 256), 256, 0, s>>>(g, k, w.from);
+      RFT_HIP(hipGetLastError(), fn);
+    }
+    RFT_HIP((g.source ? launch_tiles<DWS, RFT_ACT_NONE>(a, n, k, s) : launch_tiles<DW, RFT_ACT_NONE>(a, n, k, s)), fn);
     if (slices > 1) {
       const int64_t count = g.E * n * k;
       k_dw_sum<<<grid_xy(ceil_div(count / 4, 256)), 256, 0, s>>>(w.dw, slices, count, d_weight, a.dw_bf16,

@@ -130,8 +130,9 @@ __device__ __forceinline__ void put4(float* p, int64_t c, int64_t C, floatx4 v) 
     if (c + q < C) p[c + q] = v[q];
 }
 
-template <int FORM, int MIA, bool GLU>
+template <int FORM, int MIA, int ACT>
 __global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
+  constexpr bool GLU = ACT == RFT_ACT_SWIGLU;
   constexpr int BT = MIA == 4 ? 128 : 64;
   constexpr int WN = BT / 64;  // waves along the columns, 64 each
   constexpr int NI = BT / 32;
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
           }
           floatx4 y;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) y[q] = GLU ? silu<false>(v[q]) * u[q] : act_of<false>(g.o.act, v[q]);
+          for (int q = 0; q < 4; ++q) y[q] = GLU ? silu<false>(v[q]) * u[q] : act_of<false>(ACT, v[q]);
           if (g.o.residual) y += get4((const float*)g.o.residual + r * m, c, m);
           put4((float*)g.o.y + r * m, c, m, y);
         } else {
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(256) k_dw_sum_f32(const float* __restrict__ pa
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-template <int FORM, bool GLU>
+template <int FORM, int ACT>
 hipError_t launch(Args a, int64_t outer, int64_t across, hipStream_t s) {
   auto tiles = [&](int64_t B) {
     return FORM == DW ? a.g.E * a.slices * ceil_div(outer, B) * ceil_div(across, B)
@@ -323,16 +324,16 @@ hipError_t launch(Args a, int64_t outer, int64_t across, hipStream_t s) {
   a.most = (int)tiles(B);
   const unsigned grid = (unsigned)std::min<int64_t>(B == 128 ? 512 : 1024, ceil_div(a.most, 8) * 8);
   if (B == 128)
-    k_lin_f32<FORM, 4, GLU><<<grid, NT, 0, s>>>(a);
+    k_lin_f32<FORM, 4, ACT><<<grid, NT, 0, s>>>(a);
   else
-    k_lin_f32<FORM, 1, GLU><<<grid, NT, 0, s>>>(a);
+    k_lin_f32<FORM, 1, ACT><<<grid, NT, 0, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t linear_f32_fwd(const Groups& g, const float* x, const float* w, int64_t k, int64_t n,
-                          const Out& o, hipStream_t s) {
+                          int act, const Out& o, hipStream_t s) {
   Args a = {};
   a.g = g;
   a.a = x;
@@ -341,7 +342,9 @@ hipError_t linear_f32_fwd(const Groups& g, const float* x, const float* w, int64
   a.n = n;
   a.o = o;
   a.slices = 1;
-  return o.act == RFT_ACT_SWIGLU ? launch<FWD, true>(a, g.rows, n, s) : launch<FWD, false>(a, g.rows, n, s);
+  hipError_t err = hipSuccess;
+  by_act(act, [&](auto A) { err = launch<FWD, decltype(A)::value>(a, g.rows, n, s); });
+  return err;
 }
 
 hipError_t linear_f32_dx(const Groups& g, const float* dz, const float* w, int64_t k, int64_t n,
@@ -354,7 +357,7 @@ hipError_t linear_f32_dx(const Groups& g, const float* dz, const float* w, int64
   a.n = n;
   a.c = d_x;
   a.slices = 1;
-  return launch<DX, false>(a, g.rows, k, s);
+  return launch<DX, RFT_ACT_NONE>(a, g.rows, k, s);
 }
 
 hipError_t linear_f32_dw(const Groups& g, const float* dz, const float* x, int64_t k, int64_t n,
@@ -369,7 +372,7 @@ hipError_t linear_f32_dw(const Groups& g, const float* dz, const float* x, int64
   a.accumulate = accumulate;
   a.slices = slices;
   a.part = part;
-  const hipError_t e = launch<DW, false>(a, n, k, s);
+  const hipError_t e = launch<DW, RFT_ACT_NONE>(a, n, k, s);
   if (e != hipSuccess || slices == 1) return e;
   const int64_t count = g.E * n * k;
   k_dw_sum_f32<<<grid_xy(ceil_div(count, 256)), 256, 0, s>>>(part, slices, count, d_w, accumulate);

@@ -62,12 +62,14 @@ __device__ __forceinline__ bf16x8 fragment(const char* s, int row, int chunk) {
   return *(const bf16x8*)(s + row * 256 + ((chunk ^ (row & 15)) << 4));
 }
 
-template <bool GLU, int MT, int NS>
+template <int ACT, int MT, int NS>
 __global__ void __launch_bounds__(NT) k_few(const Few f) {
+  constexpr bool GLU = ACT == RFT_ACT_SWIGLU;
   constexpr int STAGE = (BN + MT * 16) * 256, L = 4 + MT;  // bytes; loads per wave
   __shared__ __attribute__((aligned(16))) char lds[NS * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, q4 = lane >> 4;
+  const uint32_t place = lds_at(lds);
   const int e = nth_group(f.g, blockIdx.y);
   if (e < 0) return;
   const int2 rows = rows_of(f.g, e);
@@ -99,15 +101,15 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
       xoff[i] = s < 0 ? kNone : (uint32_t)((s * f.k + xk) * 2);
     }
     auto load = [&](int t) {
-      char* const d = lds + (t % NS) * STAGE;
+      const uint32_t d = place + (t % NS) * STAGE;
       const int left = K - t * BK;
       const uint64_t step = (uint64_t)t * (BK * 2);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        load_lds(wbase + step, d + wave * 4096 + i * 1024, wk[i] < left ? woff[i] : kNone);
+        load_lds<true>(wbase + step, d + wave * 4096 + i * 1024, wk[i] < left ? woff[i] : kNone);
 #pragma unroll
       for (int i = 0; i < MT; ++i)
-        load_lds(xbase + step, d + BN * 256 + i * 4096 + wave * 1024, xk < left ? xoff[i] : kNone);
+        load_lds<true>(xbase + step, d + BN * 256 + i * 4096 + wave * 1024, xk < left ? xoff[i] : kNone);
     };
     floatx4 acc[MT];
 #pragma unroll
@@ -162,7 +164,7 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           const int64_t r = r0 + i * 16 + r16, c = col + q4 * 4;
-          if (r < rows.y && c < m) finish<true>(f.o, e, f.n, r, c, acc[i], other[i * 64 + lane]);
+          if (r < rows.y && c < m) finish<ACT>(f.o, e, f.n, r, c, acc[i], other[i * 64 + lane]);
         }
       }
       __syncthreads();
@@ -170,15 +172,16 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int64_t r = r0 + i * 16 + r16, c = col + q4 * 4;
-        if (r < rows.y && c < m) finish<false>(f.o, e, f.n, r, c, acc[i], acc[i]);
+        if (r < rows.y && c < m) finish<ACT>(f.o, e, f.n, r, c, acc[i], acc[i]);
       }
     }
   }
 }
 
 // The slices' sums, in order, and the epilogue: four columns per thread.
-template <bool GLU>
+template <int ACT>
 __global__ void __launch_bounds__(256) k_few_sum(const Few f) {
+  constexpr bool GLU = ACT == RFT_ACT_SWIGLU;
   const int64_t m = GLU ? f.n >> 1 : f.n, c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, r = blockIdx.y;
   if (c >= m) return;
   // the row's group: the last whose rows begin at or before it
@@ -198,7 +201,7 @@ __global__ void __launch_bounds__(256) k_few_sum(const Few f) {
     v += *(const floatx4*)p;
     if (GLU) u += *(const floatx4*)(p + m);
   }
-  finish<GLU>(f.o, e, f.n, r, c, v, u);
+  finish<ACT>(f.o, e, f.n, r, c, v, u);
 }
 
 }  // namespace
@@ -217,9 +220,9 @@ FewPlan linear_few_plan(const rft_groups& g, int64_t k, int64_t n, int act) {
 }
 
 hipError_t linear_few(const FewPlan& p, const Groups& g, const uint16_t* x, const uint16_t* w,
-                      int64_t k, int64_t n, const Out& o, float* ws, hipStream_t s) {
+                      int64_t k, int64_t n, int act, const Out& o, float* ws, hipStream_t s) {
   const Few f = {g, x, w, k, n, o, p.slices, ws};
-  const bool glu = o.act == RFT_ACT_SWIGLU;
+  const bool glu = act == RFT_ACT_SWIGLU;
   const dim3 grid((unsigned)((n + BN - 1) / BN), (unsigned)std::min(g.E, g.rows), (unsigned)p.slices);
   auto go = [&](auto G, auto M, auto S) {
     k_few<decltype(G)::value, decltype(M)::value, decltype(S)::value><<<grid, NT, 0, s>>>(f);
@@ -233,14 +236,11 @@ hipError_t linear_few(const FewPlan& p, const Groups& g, const uint16_t* x, cons
     else
       go(G, integral_constant<int, 4>{}, integral_constant<int, 2>{});
   };
-  glu ? by_rows(std::true_type{}) : by_rows(std::false_type{});
+  by_act(act, by_rows);
   if (p.slices > 1) {
     const int64_t m = glu ? n / 2 : n;
     const dim3 sums((unsigned)((m / 4 + 255) / 256), (unsigned)g.rows);
-    if (glu)
-      k_few_sum<true><<<sums, 256, 0, s>>>(f);
-    else
-      k_few_sum<false><<<sums, 256, 0, s>>>(f);
+    by_act(act, [&](auto A) { k_few_sum<decltype(A)::value><<<sums, 256, 0, s>>>(f); });
   }
   return hipGetLastError();
 }

@@ -2,6 +2,8 @@
 // tiles over them, and the activations.
 #pragma once
 
+#include <type_traits>
+
 #include "abi_common.h"
 
 namespace rft {
@@ -121,24 +123,43 @@ __device__ __forceinline__ uint64_t uniform(const void* p) {
   return ((uint64_t)hi << 32) | lo;
 }
 
+// Where a place in LDS lies, for the loads below.
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)p);
+}
 // 16 bytes per lane from base + v to LDS at dst + 16 lane.  Written out: in a kernel that reads
 // LDS transposed the compiler waits for every such load before each read.  It has no register
-// result, and the kernel's own waits cover it.
-__device__ __forceinline__ void load_lds(uint64_t base, char* dst, uint32_t v) {
+// result, and the kernel's own waits cover it.  NOPS: five wait states, where a vector
+// instruction may just have written the scalar registers; else one, for m0.
+template <bool NOPS>
+__device__ __forceinline__ void load_lds(uint64_t base, uint32_t dst, uint32_t v) {
 #ifdef __HIP_DEVICE_COMPILE__
   const u32x4 w = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, kSpan, 0x00020000u};
-  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)dst);
-  // five wait states: scalar registers that a vector instruction has just written
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  if constexpr (NOPS)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(dst), "v"(v), "s"(w)
+                 : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(dst), "v"(v), "s"(w)
+                 : "memory", "m0");
+#endif
+}
+// The same with four bytes per lane, to dst + 4 lane.
+__device__ __forceinline__ void load_lds4(uint64_t base, uint32_t dst, uint32_t v) {
+#ifdef __HIP_DEVICE_COMPILE__
+  const u32x4 w = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, kSpan, 0x00020000u};
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
                :
-               : "s"(at), "v"(v), "s"(w)
+               : "s"(dst), "v"(v), "s"(w)
                : "memory", "m0");
 #endif
 }
 __device__ __forceinline__ s16x4 read_tr(const char* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
-
 // ------------------------------------------------------------ activations --
 // Sigmoid.  FAST (bf16 data): exp2 of the rounded -x log2 e and a reciprocal, each good to
 // about 2^-22 where the value matters, against the 2^-9 of rounding the result.
@@ -147,8 +168,27 @@ __device__ __forceinline__ float sigmoid(float x) {
   if (FAST) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * kLog2e));
   return 1.f / (1.f + expf(-x));
 }
-// Phi by the complementary error function: 1 + erf(x) would cancel for x < 0.
-__device__ __forceinline__ float phi_cdf(float x) { return 0.5f * erfcf(-x * 0.70710678f); }
+// Phi by the complementary error function: 1 + erf(x) would cancel for x < 0.  FAST: with a =
+// |x| / sqrt 2 and t = 1 / (1 + a / 2), erfc(a) = t exp(p(t) - a^2), p fitted to ln(erfc(a)
+// exp(a^2) / t) on a in [0, 10.5] by weighted least squares (2.5e-7; 1.7e-6 with the roundings
+// for |x| < 4).
+template <bool FAST>
+__device__ __forceinline__ float phi_cdf(float x) {
+  if (!FAST) return 0.5f * erfcf(-x * 0.70710678f);
+  const float a = fabsf(x) * 0.70710678f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.5f, a, 1.f));
+  float p = 0.069136456f;
+  p = fmaf(p, t, -0.51062018f);
+  p = fmaf(p, t, 1.3867378f);
+  p = fmaf(p, t, -1.6855441f);
+  p = fmaf(p, t, 0.78946251f);
+  p = fmaf(p, t, -0.21096234f);
+  p = fmaf(p, t, 0.43327338f);
+  p = fmaf(p, t, 0.9937498f);
+  p = fmaf(p, t, -1.2652335f);
+  const float e = 0.5f * t * __builtin_amdgcn_exp2f(fmaf(-a, a, p) * kLog2e);
+  return x < 0.f ? e : 1.f - e;
+}
 
 // silu(x), with the limit 0 at -inf (x times sigmoid would be NaN there).
 template <bool FAST>
@@ -161,23 +201,23 @@ __device__ __forceinline__ float silu_slope(float x) {
   // x (1 - s) with 1 - s = s(-x): no cancellation; at infinities the limit
   return fabsf(x) > FLT_MAX ? s : fmaf(s * x, sigmoid<FAST>(-x), s);
 }
-__device__ __forceinline__ float gelu(float x) { return x == -INFINITY ? 0.f : x * phi_cdf(x); }
+template <bool FAST>
+__device__ __forceinline__ float gelu(float x) {
+  return x == -INFINITY ? 0.f : x * phi_cdf<FAST>(x);
+}
+template <bool FAST>
 __device__ __forceinline__ float gelu_slope(float x) {
   // phi(x) = exp(-x^2 / 2) / sqrt(2 pi), 0 beyond |x| = 15
   const float p = fabsf(x) < 15.f ? x * 0.39894228f * expf(-0.5f * x * x) : x != x ? x : 0.f;
-  return phi_cdf(x) + p;
-}
-template <int ACT, bool FAST>
-__device__ __forceinline__ float act1(float z) {
-  return ACT == RFT_ACT_SILU ? silu<FAST>(z) : ACT == RFT_ACT_GELU ? gelu(z) : z;
+  return phi_cdf<FAST>(x) + p;
 }
 template <bool FAST>
 __device__ __forceinline__ float act_of(int act, float z) {
-  return act == RFT_ACT_SILU ? silu<FAST>(z) : act == RFT_ACT_GELU ? gelu(z) : z;
+  return act == RFT_ACT_SILU ? silu<FAST>(z) : act == RFT_ACT_GELU ? gelu<FAST>(z) : z;
 }
 template <bool FAST>
 __device__ __forceinline__ float slope_of(int act, float z) {
-  return act == RFT_ACT_SILU ? silu_slope<FAST>(z) : act == RFT_ACT_GELU ? gelu_slope(z) : 1.f;
+  return act == RFT_ACT_SILU ? silu_slope<FAST>(z) : act == RFT_ACT_GELU ? gelu_slope<FAST>(z) : 1.f;
 }
 
 // What a forward writes.
@@ -185,7 +225,6 @@ struct Out {
   const void* bias;      // [E, n] or nullptr
   const void* residual;  // [rows, m] or nullptr
   void *y, *z;           // z nullptr: not kept
-  int act;
 };
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
@@ -198,10 +237,11 @@ __device__ __forceinline__ void store4(uint16_t* p, floatx4 v) {
 }
 
 // A forward's epilogue on bf16 data: columns [c, c + 4) of row r of group e from the product's v
-// (GLU: of the gate; u: of the other half).
-template <bool GLU>
+// (RFT_ACT_SWIGLU: of the gate; u: of the other half).
+template <int ACT>
 __device__ __forceinline__ void finish(const Out& o, int e, int64_t n, int64_t r, int64_t c, floatx4 v,
                                        floatx4 u) {
+  constexpr bool GLU = ACT == RFT_ACT_SWIGLU;
   const int64_t m = GLU ? n >> 1 : n;
   if (o.bias) {
     const uint16_t* const bias = (const uint16_t*)o.bias + e * n;
@@ -215,9 +255,69 @@ __device__ __forceinline__ void finish(const Out& o, int e, int64_t n, int64_t r
   }
   floatx4 w;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) w[q] = GLU ? silu<true>(v[q]) * u[q] : act_of<true>(o.act, v[q]);
+  for (int q = 0; q < 4; ++q) w[q] = GLU ? silu<true>(v[q]) * u[q] : act_of<true>(ACT, v[q]);
   if (o.residual) w += load4((const uint16_t*)o.residual + r * m + c);
   store4((uint16_t*)o.y + r * m + c, w);
+}
+
+// The same with eight columns (v0, v1; u0, u1), 16 bytes of a bf16 row at a time.
+__device__ __forceinline__ void load8(const uint16_t* p, floatx4& a, floatx4& b) {
+  const u32x4 w = *(const u32x4*)p;
+  a = (floatx4){__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u),
+                __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+  b = (floatx4){__uint_as_float(w[2] << 16), __uint_as_float(w[2] & 0xffff0000u),
+                __uint_as_float(w[3] << 16), __uint_as_float(w[3] & 0xffff0000u)};
+}
+__device__ __forceinline__ void store8(uint16_t* p, floatx4 a, floatx4 b) {
+  auto two = [](float x, float y) { return (uint32_t)f32_to_bf16(x) | (uint32_t)f32_to_bf16(y) << 16; };
+  *(u32x4*)p = (u32x4){two(a[0], a[1]), two(a[2], a[3]), two(b[0], b[1]), two(b[2], b[3])};
+}
+template <int ACT>
+__device__ __forceinline__ void finish8(const Out& o, int e, int64_t n, int64_t r, int64_t c, floatx4 v0,
+                                        floatx4 v1, floatx4 u0, floatx4 u1) {
+  constexpr bool GLU = ACT == RFT_ACT_SWIGLU;
+  const int64_t m = GLU ? n >> 1 : n;
+  floatx4 a, b;
+  if (o.bias) {
+    const uint16_t* const bias = (const uint16_t*)o.bias + e * n + c;
+    load8(bias, a, b);
+    v0 += a;
+    v1 += b;
+    if (GLU) {
+      load8(bias + m, a, b);
+      u0 += a;
+      u1 += b;
+    }
+  }
+  if (o.z) {
+    uint16_t* const z = (uint16_t*)o.z + r * n + c;
+    store8(z, v0, v1);
+    if (GLU) store8(z + m, u0, u1);
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    v0[q] = GLU ? silu<true>(v0[q]) * u0[q] : act_of<true>(ACT, v0[q]);
+    v1[q] = GLU ? silu<true>(v1[q]) * u1[q] : act_of<true>(ACT, v1[q]);
+  }
+  if (o.residual) {
+    load8((const uint16_t*)o.residual + r * m + c, a, b);
+    v0 += a;
+    v1 += b;
+  }
+  store8((uint16_t*)o.y + r * m + c, v0, v1);
+}
+
+// Calls f(integral_constant<int, act>).
+template <class F>
+inline void by_act(int act, F f) {
+  if (act == RFT_ACT_SILU)
+    f(std::integral_constant<int, RFT_ACT_SILU>{});
+  else if (act == RFT_ACT_GELU)
+    f(std::integral_constant<int, RFT_ACT_GELU>{});
+  else if (act == RFT_ACT_SWIGLU)
+    f(std::integral_constant<int, RFT_ACT_SWIGLU>{});
+  else
+    f(std::integral_constant<int, RFT_ACT_NONE>{});
 }
 
 // dz in the workspace, and gradients of the bias (k_linear.hip).
@@ -238,11 +338,11 @@ struct FewPlan {
 };
 FewPlan linear_few_plan(const rft_groups& g, int64_t k, int64_t n, int act);
 hipError_t linear_few(const FewPlan& p, const Groups& g, const uint16_t* x, const uint16_t* w,
-                      int64_t k, int64_t n, const Out& o, float* ws, hipStream_t s);
+                      int64_t k, int64_t n, int act, const Out& o, float* ws, hipStream_t s);
 
 // Entry points of the fp32 kernels (k_linear_f32.hip).
 hipError_t linear_f32_fwd(const Groups& g, const float* x, const float* w, int64_t k, int64_t n,
-                          const Out& o, hipStream_t s);
+                          int act, const Out& o, hipStream_t s);
 hipError_t linear_f32_dx(const Groups& g, const float* dz, const float* w, int64_t k, int64_t n,
                          float* d_x, hipStream_t s);
 hipError_t linear_f32_dw(const Groups& g, const float* dz, const float* x, int64_t k, int64_t n,
