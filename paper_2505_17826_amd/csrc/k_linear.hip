@@ -25,6 +25,7 @@ namespace {
 
 enum { FWD = 0, DX = 1, DW = 2, DWS = 3 };  // DWS: DW with a source
 constexpr int BK = 64, NT = 256;
+constexpr int kStart = 8;  // stages that a tile takes for its start and its stores, about
 
 struct Args {
   Groups g;
@@ -135,24 +136,28 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
   constexpr int RA = (AC ? 2 : 1) * MI, RD = RA + (BC ? 2 : 1) * NJ;  // reads per stage
   constexpr int PD = MI * NJ;                                         // products
   __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
-  __shared__ int tab[FORM == DW ? 1 : kMaxGroups + 1], sh[NT / 64];
+  __shared__ int tab[kMaxGroups + 1], sh[NT / 64];
   __shared__ uint32_t ring[SRC ? NT / 64 : 1][4][BK];  // DW with a source: offsets of stages' rows
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = (wid >> 1) * (16 * MI), wn = (wid & 1) * (16 * NJ);
   const int r16 = lane & 15, q4 = lane >> 4;
   const int64_t k = g.k, n = g.n;
-  int items;
-  if constexpr (FORM == DW) {
-    items = g.most;
-  } else {
-    tile_table<NT, BM>(g.g, g.tn, g.most, tab, sh);
-    items = __builtin_amdgcn_readfirstlane(tab[g.g.E]);
-  }
   // Blocks go round the eight XCDs, each with an L2 of its own: XCD x takes the x-th eighth of
-  // the tiles.
-  const int xcd = blockIdx.x & 7, per = (items + 7) / 8;
-  const int last = min(items, (xcd + 1) * per);
+  // the tiles, by their costs where those go by the rows of the group (DW).
+  const int xcd = blockIdx.x & 7;
+  int first, last;
+  if constexpr (FORM == DW) {
+    const int each = (int)((n + BM - 1) / BM) * g.tn * g.slices;
+    tile_table<NT, BK>(g.g, 1, kStart * g.slices, 1 << 30, tab, sh);
+    first = share_of(tab, g.g.E, each, xcd, 8);
+    last = share_of(tab, g.g.E, each, xcd + 1, 8);
+  } else {
+    tile_table<NT, BM>(g.g, g.tn, 0, g.most, tab, sh);
+    const int items = __builtin_amdgcn_readfirstlane(tab[g.g.E]), per = (items + 7) / 8;
+    first = xcd * per;
+    last = min(items, first + per);
+  }
 
   struct Tile {
     int e, m0, n0, slice, y;  // group, first row and column of the tile, end of the group's rows
@@ -174,7 +179,7 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
   auto set = [&](int item, Tile& t) {
     int ti, tj;
     t.slice = 0;
-    if constexpr (FORM == DW) {
+    if constexpr (FORM == DW) {  // group by group, slice by slice
       const int tm = (int)((n + BM - 1) / BM), each = tm * g.tn;
       t.e = item / each;
       tile_at(item - t.e * each, tm, g.tn, ti, tj);
@@ -227,6 +232,7 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
       if constexpr (SRC) {
         B.step = 0;
         from = uniform(g.from + t.x);
+        fs = 0;
         load_from();
         load_from();
         load_from();
@@ -311,28 +317,28 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
   };
 
   Tile t;
-  int item = xcd * per + (blockIdx.x >> 3);
+  int item = first + (blockIdx.x >> 3);
   const int stride = gridDim.x >> 3;
-  auto next = [&]() {  // sets the next tile and issues its first stages
+  auto next = [&]() {  // sets the next tile and issues its first stage
     for (; item < last; item += stride) {
       if (!set(item, t)) continue;
       item += stride;
-      // (what the operands' set-up read has landed)
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int x = 0; x < L; ++x) load_one(std::true_type{}, p * STAGE, x);
+      for (int x = 0; x < L; ++x) load_one(std::true_type{}, 0, x);
       return true;
     }
     return false;
   };
-  while (next()) {
+  bool more = next();
+  while (more) {
+#pragma unroll
+    for (int x = 0; x < L; ++x) load_one(std::true_type{}, STAGE, x);
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
     const int nk = (K + BK - 1) / BK;
-    wait_vm<L + (SRC ? 1 : 0)>();  // stage 0
+    wait_vm<L + (SRC ? 1 : 0)>();  // stage 0 (and the stores of the tile before)
     barrier_lds();
 #pragma unroll
     for (int x = 0; x < RD; ++x) read_one(0, lds, x);
@@ -382,26 +388,30 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
     wait_vm<0>();
     wait_lds();
     barrier_lds();  // no load is under way, the stages are free
-    // Element q of tile (i, j) is row 16 i + r16, column 16 j + 4 q4 + q of the wave's part.  64 rows
-    // at a time go through LDS (16-byte chunk c of row r at c ^ (r & 15)), so that a lane has eight
-    // columns of a row and a row is written in whole cache lines.
-    float* const mine = (float*)(lds + wid * (STAGE / 2));
+    const Tile d = t;
+    more = next();
+    // Element q of tile (i, j) is row 16 i + r16, column 16 j + 4 q4 + q of the wave's part.  32 rows
+    // at a time go through the second stage's place in LDS (16-byte chunk c of row r at c ^ (r &
+    // 15)), so that a lane has eight columns of a row and a row is written in whole cache lines;
+    // the next tile's first stage is on its way to the first one's.
+    float* const mine = (float*)(lds + STAGE + wid * (STAGE / 4));
     constexpr int CH = 4 * NJ;  // chunks per row
 #pragma unroll
-    for (int h = 0; h < MI / 4; ++h) {
+    for (int h = 0; h < MI / 2; ++h) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
-          *(floatx4*)(mine + ((i * 16 + r16) * CH + ((j * 4 + q4) ^ r16)) * 4) = acc[h * 4 + i][j];
+          *(floatx4*)(mine + ((i * 16 + r16) * CH + ((j * 4 + q4) ^ r16)) * 4) = acc[h * 2 + i][j];
       wait_lds();
       __builtin_amdgcn_wave_barrier();
       constexpr int OC = GLU ? 8 * NJ : 16 * NJ, LR = OC / 8;  // columns out; lanes per row
       const int oc = (lane % LR) * 8;
-      const int64_t c = (GLU ? (t.n0 + wn) / 2 : t.n0 + wn) + oc;
-#pragma unroll 1
-      for (int row = lane / LR; row < 64; row += 64 / LR) {
-        const int64_t o = t.m0 + wm + h * 64 + row;
+      const int64_t c = (GLU ? (d.n0 + wn) / 2 : d.n0 + wn) + oc;
+#pragma unroll 4
+      for (int row0 = 0; row0 < 32; row0 += 64 / LR) {
+        const int row = row0 + lane / LR;
+        const int64_t o = d.m0 + wm + h * 32 + row;
         auto get = [&](int col) {
           return *(const floatx4*)(mine + (row * CH + ((col >> 2) ^ (row & 15))) * 4);
         };
@@ -409,20 +419,20 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
         const int v = GLU ? (oc >> 4) * 32 + (oc & 15) : oc;
         const floatx4 v0 = get(v), v1 = get(v + 4);
         if constexpr (FORM == FWD) {
-          if (t.x + o < t.y && c < (GLU ? n >> 1 : n)) {
+          if (d.x + o < d.y && c < (GLU ? n >> 1 : n)) {
             floatx4 u0 = v0, u1 = v1;
             if (GLU) {
               u0 = get(v + 16);
               u1 = get(v + 20);
             }
-            finish8<ACT>(g.o, t.e, n, t.x + o, c, v0, v1, u0, u1);
+            finish8<ACT>(g.o, d.e, n, d.x + o, c, v0, v1, u0, u1);
           }
         } else if constexpr (FORM == DX) {
-          if (t.x + o < t.y && c < k) store8(g.dx + (t.x + o) * k + c, v0, v1);
+          if (d.x + o < d.y && c < k) store8(g.dx + (d.x + o) * k + c, v0, v1);
         } else if (o < n && c < k) {
-          const int64_t at = (t.e * n + o) * k + c;
+          const int64_t at = (d.e * n + o) * k + c;
           if (g.slices > 1) {
-            floatx4* const p = (floatx4*)(g.part + (int64_t)t.slice * g.g.E * n * k + at);
+            floatx4* const p = (floatx4*)(g.part + (int64_t)d.slice * g.g.E * n * k + at);
             p[0] = v0;
             p[1] = v1;
           } else if (g.dw_bf16) {

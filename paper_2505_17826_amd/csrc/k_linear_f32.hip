@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
   if constexpr (FORM == DW) {
     items = g.most;
   } else {
-    tile_table<NT, BT>(g.g, g.tn, g.most, tab, sh);
+    tile_table<NT, BT>(g.g, g.tn, 0, g.most, tab, sh);
     items = tab[g.g.E];
   }
   const int xcd = blockIdx.x & 7, per = (items + 7) / 8;

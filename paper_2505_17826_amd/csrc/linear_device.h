@@ -35,11 +35,12 @@ __device__ __forceinline__ int64_t source_of(const Groups& g, int r) {
   return s >= 0 && t < g.source_rows ? t : -1;
 }
 
-// Tiles of BM rows over the groups, `across` tiles wide: tab[e] = tiles of the groups before e
+// Tiles of BM rows over the groups (and `more` for each), `across` tiles wide: tab[e] = tiles of the groups before e
 // (tab[E]: all, at most `most`: invalid offsets could claim rows more than once).  By every
 // thread of a block of NT; sh: NT / 64 entries.
 template <int NT, int BM>
-__device__ __forceinline__ void tile_table(const Groups& g, int across, int most, int* tab, int* sh) {
+__device__ __forceinline__ void tile_table(const Groups& g, int across, int more, int most, int* tab,
+                                           int* sh) {
   constexpr int PER = kMaxGroups / NT, NW = NT / 64;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   int64_t c[PER], sum = 0;
@@ -49,7 +50,7 @@ __device__ __forceinline__ void tile_table(const Groups& g, int across, int most
     c[i] = 0;
     if (e < g.E) {
       const int2 r = rows_of(g, e);
-      c[i] = (int64_t)((r.y - r.x + BM - 1) / BM) * across;
+      c[i] = (int64_t)((r.y - r.x + BM - 1) / BM + more) * across;
     }
     sum = min(sum + c[i], (int64_t)most);
   }
@@ -73,6 +74,18 @@ __device__ __forceinline__ void tile_table(const Groups& g, int across, int most
     if (e == g.E - 1) tab[g.E] = (int)min(at, (int64_t)most);
   }
   __syncthreads();
+}
+
+// First of the items (`each` per group, all of a group of one cost: stages of its rows, and
+// kStart more for what a tile takes besides) of the p-th of `parts` equal shares of the cost; cost:
+// a table of the groups' costs (tile_table with BM = 64 rows and `more` = kStart).  By whole waves.
+__device__ __forceinline__ int group_of(const int* tab, int E, int item);
+__device__ __forceinline__ int share_of(const int* cost, int E, int each, int p, int parts) {
+  const int64_t at = (int64_t)cost[E] * p / parts;  // in costs of one tile of every group
+  if (p >= parts) return E * each;
+  const int e = group_of(cost, E, (int)at);
+  const int64_t w = max(cost[e + 1] - cost[e], 1);
+  return __builtin_amdgcn_readfirstlane(e * each + (int)((((int64_t)cost[E] * p - (int64_t)cost[e] * parts) * each) / (w * parts)));
 }
 
 // The group whose tiles hold `item` < tab[E]: the last e with tab[e] <= item.  By whole waves.
@@ -232,8 +245,10 @@ __device__ __forceinline__ floatx4 load4(const uint16_t* p) {
   const u16x4 h = *(const u16x4*)p;
   return (floatx4){bf16_to_f32(h[0]), bf16_to_f32(h[1]), bf16_to_f32(h[2]), bf16_to_f32(h[3])};
 }
+// Rounded to nearest even by the conversion instruction (two at a time), as f32_to_bf16 does.
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void store4(uint16_t* p, floatx4 v) {
-  *(u16x4*)p = (u16x4){f32_to_bf16(v[0]), f32_to_bf16(v[1]), f32_to_bf16(v[2]), f32_to_bf16(v[3])};
+  *(bf16x4*)p = __builtin_convertvector(v, bf16x4);
 }
 
 // A forward's epilogue on bf16 data: columns [c, c + 4) of row r of group e from the product's v
@@ -269,8 +284,8 @@ __device__ __forceinline__ void load8(const uint16_t* p, floatx4& a, floatx4& b)
                 __uint_as_float(w[3] << 16), __uint_as_float(w[3] & 0xffff0000u)};
 }
 __device__ __forceinline__ void store8(uint16_t* p, floatx4 a, floatx4 b) {
-  auto two = [](float x, float y) { return (uint32_t)f32_to_bf16(x) | (uint32_t)f32_to_bf16(y) << 16; };
-  *(u32x4*)p = (u32x4){two(a[0], a[1]), two(a[2], a[3]), two(b[0], b[1]), two(b[2], b[3])};
+  const bf16x4 x = __builtin_convertvector(a, bf16x4), y = __builtin_convertvector(b, bf16x4);
+  *(bf16x8*)p = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 template <int ACT>
 __device__ __forceinline__ void finish8(const Out& o, int e, int64_t n, int64_t r, int64_t c, floatx4 v0,

@@ -216,6 +216,17 @@ def test_backward_sizes(k, n, dt):
     check_backward(Case([37, 0, 140], k, n, "none", dt, seed=k), dw_dtype=F32)
 
 
+def test_many_tiles_of_sources():
+    """Several tiles per block of both tile sizes, each with its own rows of the tokens."""
+    g = torch.Generator().manual_seed(13)
+    for counts, k, n in (([300, 0, 70, 513], 1032, 4104), ([100] * 40, 264, 528)):
+        rows, tokens, div = sum(counts), 61, 3
+        source = torch.randint(0, tokens * div, (rows,), generator=g, dtype=torch.int32)
+        c = Case(counts, k, n, "none", BF, source=source, div=div, tokens=tokens, seed=k)
+        check_forward(c, want_z=False)
+        check_backward(c, dw_dtype=F32)
+
+
 @pytest.mark.parametrize("dt", (BF, F32))
 def test_sources(dt):
     """Rows taken from the tokens by slots, some of them no row of x."""
