@@ -506,18 +506,15 @@ __device__ __forceinline__ void store_v(void* p, int64_t at, const float (&v)[V]
     else
       ((float*)p)[at] = v[0];
   } else if constexpr (BF16) {
-    u32x4 w;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      w[q] = (uint32_t)f32_to_bf16(v[2 * q]) | (uint32_t)f32_to_bf16(v[2 * q + 1]) << 16;
-    *(u32x4*)((uint16_t*)p + at) = w;
+    store8((uint16_t*)p + at, (floatx4){v[0], v[1], v[2], v[3]}, (floatx4){v[4], v[5], v[6], v[7]});
   } else {
     *(floatx4*)((float*)p + at) = (floatx4){v[0], v[1], v[2], v[3]};
   }
 }
 
-template <bool BF16, int V>
+template <bool BF16, int V, bool BIAS>
 __global__ void __launch_bounds__(256) k_dz(const Groups g, const Dz d, int slices, double* part) {
+  constexpr int R = V == 1 ? 4 : 2;  // rows whose loads are under way
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int e = blockIdx.y, slice = blockIdx.z;
   const bool glu = d.act == RFT_ACT_SWIGLU;
@@ -530,31 +527,40 @@ __global__ void __launch_bounds__(256) k_dz(const Groups g, const Dz d, int slic
 #pragma unroll
   for (int q = 0; q < V; ++q) s0[q] = s1[q] = 0.f;
   if (c < m) {
-    for (int64_t i = a + w; i < b; i += 4) {
-      float dy[V], z[V], u[V];
-      load_v<BF16, V>(d.dy, i * m + c, dy);
-      if (d.act != RFT_ACT_NONE) load_v<BF16, V>(d.z, i * d.n + c, z);
-      if (glu) load_v<BF16, V>(d.z, i * d.n + m + c, u);
+    for (int64_t i0 = a + w; i0 < b; i0 += 4 * R) {
+      float dy[R][V], z[R][V], u[R][V];
 #pragma unroll
-      for (int q = 0; q < V; ++q) {
-        if (glu) {
-          const float g1 = dy[q] * u[q] * silu_slope<BF16>(z[q]);
-          u[q] = dy[q] * silu<BF16>(z[q]);
-          s1[q] += u[q];
-          dy[q] = g1;
-        } else if (d.act != RFT_ACT_NONE) {
-          dy[q] *= slope_of<BF16>(d.act, z[q]);
-        }
-        s0[q] += dy[q];
+      for (int x = 0; x < R; ++x) {
+        const int64_t i = min(i0 + 4 * x, b - 1);  // (a row past the end is the last one, not used)
+        load_v<BF16, V>(d.dy, i * m + c, dy[x]);
+        if (d.act != RFT_ACT_NONE) load_v<BF16, V>(d.z, i * d.n + c, z[x]);
+        if (glu) load_v<BF16, V>(d.z, i * d.n + m + c, u[x]);
       }
-      if (d.dz) {
-        store_v<BF16, V>(d.dz, i * d.n + c, dy);
-        if (glu) store_v<BF16, V>(d.dz, i * d.n + m + c, u);
+#pragma unroll
+      for (int x = 0; x < R; ++x) {
+        const int64_t i = i0 + 4 * x;
+        if (i >= b) break;
+#pragma unroll
+        for (int q = 0; q < V; ++q) {
+          if (glu) {
+            const float g1 = dy[x][q] * u[x][q] * silu_slope<BF16>(z[x][q]);
+            u[x][q] = dy[x][q] * silu<BF16>(z[x][q]);
+            if (BIAS) s1[q] += u[x][q];
+            dy[x][q] = g1;
+          } else if (d.act != RFT_ACT_NONE) {
+            dy[x][q] *= slope_of<BF16>(d.act, z[x][q]);
+          }
+          if (BIAS) s0[q] += dy[x][q];
+        }
+        if (d.dz) {
+          store_v<BF16, V>(d.dz, i * d.n + c, dy[x]);
+          if (glu) store_v<BF16, V>(d.dz, i * d.n + m + c, u[x]);
+        }
       }
     }
   }
-  if (!d.d_bias) return;
-  __shared__ float sum[4][2][64 * V];
+  if constexpr (!BIAS) return;
+  __shared__ float sum[4][2][BIAS ? 64 * V : 1];
 #pragma unroll
   for (int q = 0; q < V; ++q) {
     sum[w][0][q * 64 + lane] = s0[q];
@@ -651,7 +657,11 @@ hipError_t launch_tiles(const Args& a, int64_t outer, int64_t across, hipStream_
     return FORM >= DW ? a.g.E * a.slices * ceil_div(outer, bm) * ceil_div(across, bn)
                       : (outer / bm + a.g.E) * ceil_div(across, bn);
   };
-  if (tiles(256, 256) >= 256)
+  // By rounds; one of small tiles, half the work of one of large ones, takes 0.65 of its time.
+  auto time = [&](int64_t b, int per) {  // of a group's last tile half is taken to be there
+    return rounds(FORM >= DW ? tiles(b, b) : tiles_expected(outer, a.g.E, b) * ceil_div(across, b), per);
+  };
+  if (time(256, 1) <= 0.65 * time(128, 2))
     return launch_lin<FORM, 8, 8, ACT>(a, tiles(256, 256), across, s);
   return launch_lin<FORM, 4, 4, ACT>(a, tiles(128, 128), across, s);
 }
@@ -776,12 +786,20 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
     const bool wide = bf || (m % 4 == 0 && n % 4 == 0 && aligned16(dy) && aligned16(z));
     const int V = bf ? 8 : wide ? 4 : 1, sl = dz_slices(*groups, m, V);
     const dim3 grid((unsigned)ceil_div(m, 64 * V), (unsigned)g.E, (unsigned)sl);
+    auto go = [&](auto B, auto W) {
+      constexpr bool bf16 = decltype(B)::value;
+      constexpr int v = decltype(W)::value;
+      if (d_bias)
+        k_dz<bf16, v, true><<<grid, 256, 0, s>>>(g, d, sl, w.bias);
+      else
+        k_dz<bf16, v, false><<<grid, 256, 0, s>>>(g, d, sl, w.bias);
+    };
     if (bf)
-      k_dz<true, 8><<<grid, 256, 0, s>>>(g, d, sl, w.bias);
+      go(std::true_type{}, std::integral_constant<int, 8>{});
     else if (wide)
-      k_dz<false, 4><<<grid, 256, 0, s>>>(g, d, sl, w.bias);
+      go(std::false_type{}, std::integral_constant<int, 4>{});
     else
-      k_dz<false, 1><<<grid, 256, 0, s>>>(g, d, sl, w.bias);
+      go(std::false_type{}, std::integral_constant<int, 1>{});
     RFT_HIP(hipGetLastError(), fn);
     if (d_bias && sl > 1) {
       k_bias_sum<<<(unsigned)ceil_div(g.E * n, 256), 256, 0, s>>>(w.bias, sl, g.E * n, d_bias, accumulate);

@@ -131,11 +131,13 @@ __device__ __forceinline__ void put4(float* p, int64_t c, int64_t C, floatx4 v) 
 }
 
 template <int FORM, int MIA, int ACT>
-__global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
+__global__ void __launch_bounds__(NT, MIA == 4 ? 2 : FORM == DX || ACT == RFT_ACT_SWIGLU ? 3 : 4) k_lin_f32(const Args g) {
   constexpr bool GLU = ACT == RFT_ACT_SWIGLU;
   constexpr int BT = MIA == 4 ? 128 : 64;
   constexpr int WN = BT / 64;  // waves along the columns, 64 each
   constexpr int NI = BT / 32;
+  // steps whose loads are under way: the small tile's products are shorter than a load
+  constexpr int PF = MIA == 4 ? 1 : 2;
   __shared__ __attribute__((aligned(16))) float lds[2][2][BK * BT];
   __shared__ int tab[kMaxGroups + 1], sh[NT / 64];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -178,7 +180,7 @@ __global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
     const int64_t half = n / 2;
     const float* const we = FORM == DW ? g.b : g.b + e * n * k;
     const int K = FORM == FWD ? (int)k : FORM == DX ? (int)n : rows.y - rows.x;
-    LoadK<BT> ka, kb;
+    LoadK<BT> ka, kb_;
     LoadR<BT> ra, rb;
     if constexpr (FORM != DW) {
       ka.start([&](int o) -> const float* {
@@ -192,7 +194,7 @@ __global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
       ra.start();
     }
     if constexpr (FORM == FWD) {
-      kb.start([&](int o) -> const float* {
+      kb_.start([&](int o) -> const float* {
         if (GLU) {  // 16 columns of the gate, then the same 16 of the other half
           const int64_t c = (n0 >> 1) + (o >> 5) * 16 + (o & 15);
           return c < half ? we + (c + (o >> 4 & 1) * half) * k : nullptr;
@@ -202,22 +204,22 @@ __global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
     } else {
       rb.start();
     }
-    floatx4 va[NI], vb[NI];
-    auto fetch = [&](int k0) {
+    floatx4 va[PF][NI], vb[PF][NI];
+    auto fetch = [&](int k0, int p) {
       if constexpr (FORM != DW) {
-        ka.load(k0, K, va);
+        ka.load(k0, K, va[p]);
       } else {
-        ra.load([&](int r) { return g.a + (rows.x + r) * n; }, m0, n, k0, K, va);
+        ra.load([&](int r) { return g.a + (rows.x + r) * n; }, m0, n, k0, K, va[p]);
       }
       if constexpr (FORM == FWD) {
-        kb.load(k0, K, vb);
+        kb_.load(k0, K, vb[p]);
       } else if constexpr (FORM == DX) {
-        rb.load([&](int r) { return we + r * k; }, n0, k, k0, K, vb);
+        rb.load([&](int r) { return we + r * k; }, n0, k, k0, K, vb[p]);
       } else {
         rb.load([&](int r) -> const float* {
           const int64_t s = source_of(g.g, rows.x + r);
           return s < 0 ? nullptr : we + s * k;
-        }, n0, k, k0, K, vb);
+        }, n0, k, k0, K, vb[p]);
       }
     };
     floatx4 acc[MIA][4];
@@ -225,15 +227,21 @@ __global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
     for (int i = 0; i < MIA; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
-    if (K > 0) fetch(0);
-    for (int k0 = 0; k0 < K; k0 += BK) {
+#pragma unroll
+    for (int p = 0; p < PF; ++p)
+      if (p * BK < K) fetch(p * BK, p);
+    for (int kb = 0; kb < K; kb += PF * BK) {
+#pragma unroll
+     for (int p = 0; p < PF; ++p) {
+      const int k0 = kb + p * BK;
+      if (k0 >= K) break;
       const int st = (k0 / BK) & 1;
-      if constexpr (FORM != DW) ka.put(lds[st][0], va); else ra.put(lds[st][0], va);
-      if constexpr (FORM == FWD) kb.put(lds[st][1], vb); else rb.put(lds[st][1], vb);
+      if constexpr (FORM != DW) ka.put(lds[st][0], va[p]); else ra.put(lds[st][0], va[p]);
+      if constexpr (FORM == FWD) kb_.put(lds[st][1], vb[p]); else rb.put(lds[st][1], vb[p]);
       // this step's stage is complete; the other one is free once every wave is past its
       // products, i.e. at the next step's barrier
       __syncthreads();
-      if (k0 + BK < K) fetch(k0 + BK);
+      if (k0 + PF * BK < K) fetch(k0 + PF * BK, p);
       const float *const As = lds[st][0], *const Bs = lds[st][1];
       // the fragments of four K are read while the previous four's products run
       float a[2][MIA], b[2][4];
@@ -257,6 +265,7 @@ __global__ void __launch_bounds__(NT, 2) k_lin_f32(const Args g) {
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[kg & 1][j], a[kg & 1][i], acc[i][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
+     }
     }
     __syncthreads();  // the stages are free for the next tile
     // element q of tile (i, j): row m0 + wm + 16 i + r16, column n0 + wn + 16 j + 4 q4 + q
@@ -319,7 +328,12 @@ hipError_t launch(Args a, int64_t outer, int64_t across, hipStream_t s) {
     return FORM == DW ? a.g.E * a.slices * ceil_div(outer, B) * ceil_div(across, B)
                       : (outer / B + a.g.E) * ceil_div(across, B);
   };
-  const int B = tiles(128) >= 256 ? 128 : 64;
+  // By rounds; one of small tiles, half the work of one of large ones, takes 0.6 of its time (520
+  // tiles of 128 x 128 141 us, as tiles of 64 x 64 102; 768 tiles 250 and 290).
+  auto time = [&](int64_t b, int per) {  // of a group's last tile half is taken to be there
+    return rounds(FORM == DW ? tiles(b) : tiles_expected(outer, a.g.E, b) * ceil_div(across, b), per);
+  };
+  const int B = time(128, 2) < 0.6 * time(64, 4) ? 128 : 64;
   a.tn = (int)ceil_div(across, B);
   a.most = (int)tiles(B);
   const unsigned grid = (unsigned)std::min<int64_t>(B == 128 ? 512 : 1024, ceil_div(a.most, 8) * 8);

@@ -344,6 +344,17 @@ struct Dz {
   int64_t n;
 };
 
+// Time of `tiles` tiles, `per` to a CU at a time, in rounds of all 256 CUs; where a last round
+// leaves half of a CU's places empty, the others have it to themselves.
+inline double rounds(int64_t tiles, int per) {
+  const int64_t slots = 256 * per, rest = tiles % slots;
+  return (double)(tiles / slots) + (rest == 0 ? 0.0 : per > 1 && rest <= slots / 2 ? 0.6 : 1.0);
+}
+
+inline int64_t tiles_expected(int64_t rows, int groups, int64_t b) {
+  return groups == 1 ? (rows + b - 1) / b : rows / b + (groups + 1) / 2;
+}
+
 // Few rows per group, bf16 (k_linear_few.hip).
 struct FewPlan {
   bool fits;
