@@ -25,7 +25,7 @@ namespace {
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMaxExperts = 1024, kMaxTopK = 16;
 constexpr int64_t kFewSlots = 16384;
-constexpr int64_t kBlockSlots = 8192;
+constexpr int64_t kBlockSlots = 8192;  // both: at most 64 kRun for a wave
 
 struct Order {
   const int32_t* ids;  // expert_ids (sort) or nullptr
@@ -56,21 +56,31 @@ __device__ __forceinline__ int block_scan(int v, int* sh, int* total) {
   return before + s - v;
 }
 
-// The wave's slots [a, b): counts per expert into h[E] (this wave's, in LDS).
-__device__ __forceinline__ void count_slots(const Order& o, int64_t a, int64_t b, int* h) {
+// The ids of the wave's slots [a, b), 64 kRun at most: all loads go out before the first is used.
+constexpr int kRun = 16;
+static_assert(kFewSlots <= kSortWaves * 64 * kRun && kBlockSlots <= kFewSlots, "a wave's run");
+__device__ __forceinline__ void load_ids(const Order& o, int64_t a, int64_t b, int (&id)[kRun]) {
   const int lane = threadIdx.x & 63;
-  for (int64_t i = a; i < b; i += 64) {
-    const int e = i + lane < b ? o.ids[i + lane] : -1;
-    if ((unsigned)e < (unsigned)o.E) atomicAdd(h + e, 1);
-  }
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) id[i] = a + i * 64 + lane < b ? o.ids[a + i * 64 + lane] : -1;
+}
+
+// Counts per expert into h[E] (this wave's, in LDS).
+__device__ __forceinline__ void count_slots(const Order& o, const int (&id)[kRun], int* h) {
+#pragma unroll
+  for (int i = 0; i < kRun; ++i)
+    if ((unsigned)id[i] < (unsigned)o.E) atomicAdd(h + id[i], 1);
 }
 
 // The wave's slots [a, b) to their places; h[e]: the next place of expert e for this wave.
-__device__ __forceinline__ void place_slots(const Order& o, int64_t a, int64_t b, int* h) {
+__device__ __forceinline__ void place_slots(const Order& o, int64_t a, int64_t b, const int (&id)[kRun],
+                                            int* h) {
   const int lane = threadIdx.x & 63;
-  for (int64_t i = a; i < b; i += 64) {
-    const bool in = i + lane < b;
-    const int e = in ? o.ids[i + lane] : -1;
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) {
+    const int64_t s = a + i * 64 + lane;
+    if (a + i * 64 >= b) break;
+    const int e = id[i];
     const bool has = (unsigned)e < (unsigned)o.E;
     uint64_t peers = __builtin_amdgcn_ballot_w64(has);
     for (int q = 0; q < o.bits; ++q) {
@@ -82,8 +92,8 @@ __device__ __forceinline__ void place_slots(const Order& o, int64_t a, int64_t b
     __builtin_amdgcn_wave_barrier();
     if (has && below == 0) h[e] += __builtin_popcountll(peers);
     __builtin_amdgcn_wave_barrier();
-    if (has) o.slots[at] = (int32_t)(i + lane);
-    if (in) o.places[i + lane] = at;
+    if (has) o.slots[at] = (int32_t)s;
+    if (s < b) o.places[s] = at;
   }
 }
 
@@ -130,11 +140,13 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_few(const Order o) {
   int64_t a, b;
   wave_run(0, o.n, a, b);
   int* const mine = h + (threadIdx.x >> 6) * o.E;
-  count_slots(o, a, b, mine);
+  int id[kRun];
+  load_ids(o, a, b, id);
+  count_slots(o, id, mine);
   __syncthreads();
   int n;
   first_places(o, h, nullptr, nullptr, 0, true, sh, &n);
-  place_slots(o, a, b, mine);
+  place_slots(o, a, b, id, mine);
   for (int64_t i = n + threadIdx.x; i < o.n; i += kSortThreads) o.slots[i] = -1;
 }
 
@@ -145,7 +157,9 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(const Order o, int3
   __syncthreads();
   int64_t a, b;
   wave_run(blockIdx.x * kBlockSlots, min(o.n, (blockIdx.x + 1) * kBlockSlots), a, b);
-  count_slots(o, a, b, h);
+  int id[kRun];
+  load_ids(o, a, b, id);
+  count_slots(o, id, h);
   __syncthreads();
   for (int i = threadIdx.x; i < o.E; i += kSortThreads) part[i * blocks + blockIdx.x] = h[i];
 }
@@ -177,11 +191,13 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_place(const Order o, cons
   int64_t a, b;
   wave_run(blockIdx.x * kBlockSlots, min(o.n, (blockIdx.x + 1) * kBlockSlots), a, b);
   int* const mine = h + (threadIdx.x >> 6) * o.E;
-  count_slots(o, a, b, mine);
+  int id[kRun];
+  load_ids(o, a, b, id);
+  count_slots(o, id, mine);
   __syncthreads();
   int n;
   first_places(o, h, total, part + blockIdx.x, blocks, blockIdx.x == 0, sh, &n);
-  place_slots(o, a, b, mine);
+  place_slots(o, a, b, id, mine);
   const int64_t end = min(o.n, (blockIdx.x + 1) * kBlockSlots);
   for (int64_t i = max((int64_t)n, blockIdx.x * kBlockSlots) + threadIdx.x; i < end; i += kSortThreads)
     o.slots[i] = -1;

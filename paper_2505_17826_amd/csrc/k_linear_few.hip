@@ -209,9 +209,15 @@ __global__ void __launch_bounds__(256) k_few_sum(const Few f) {
 FewPlan linear_few_plan(const rft_groups& g, int64_t k, int64_t n, int act) {
   FewPlan p = {};
   const int64_t average = (g.rows + g.n_groups - 1) / g.n_groups;
-  p.fits = average <= 64 && g.rows <= 65535;
-  p.tiles = g.rows <= 16 || average <= 8 ? 1 : average <= 32 ? 2 : 4;
   const int64_t blocks = (n + BN - 1) / BN * std::min<int64_t>(g.n_groups, g.rows);
+  // Against tiles of 128 x 128 (64 groups, 1536 x 1536; us): 25 rows on average 57 and 79, 40 rows 78
+  // and 79, 64 rows 92 and 67; one group, 3584 x 4096: 128 rows 21 and 30, 256 rows 32 and 30,
+  // 3584 x 18944: 64 rows 31 and 31, 128 rows 60 and 33.
+  p.fits = (average <= 40 || (average <= 128 && blocks < 128)) && g.rows <= 65535;
+  // A group with more rows than a block takes at a time has its weight read again: with an uneven
+  // load of 25 rows on average 57 us at four tiles, 66 at two.
+  const int64_t likely = g.n_groups == 1 ? g.rows : 2 * average;
+  p.tiles = likely <= 16 ? 1 : likely <= 32 ? 2 : 4;
   p.slices = 1;
   if (blocks > 0 && blocks < 128)
     p.slices = (int)std::max<int64_t>(1, std::min<int64_t>({512 / blocks, (k + BK - 1) / BK / 4, 16}));
