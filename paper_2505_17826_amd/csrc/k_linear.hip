@@ -27,6 +27,12 @@ enum { FWD = 0, DX = 1, DW = 2, DWS = 3 };  // DWS: DW with a source
 constexpr int BK = 64, NT = 256;
 constexpr int kStart = 8;  // stages that a tile takes for its start and its stores, about
 
+// The tiles that are left after whole rounds of all CUs, [full, full + rest), each in `slices` of
+// the summed index, which k_tail adds; slices 1: there are none such.
+struct Tail {
+  int full, rest, slices;
+};
+
 struct Args {
   Groups g;
   const uint16_t *a, *b;  // FWD: x, W; DX: dz, W; DW: dz, x
@@ -40,6 +46,7 @@ struct Args {
   int slices;             // DW: of a group's rows; > 1: sums to part [slices, E, n, k]
   float* part;
   const uint32_t* from;   // DW with a source: byte offsets of the rows of x (k_from)
+  Tail tail;              // one group of all rows: sums to part [rest, slices, BM, BN]
 };
 
 // One operand of a tile (its outer index), as a wave loads it: P pieces of 1 KiB per stage of 64
@@ -144,10 +151,15 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
   const int r16 = lane & 15, q4 = lane >> 4;
   const int64_t k = g.k, n = g.n;
   // Blocks go round the eight XCDs, each with an L2 of its own: XCD x takes the x-th eighth of
-  // the tiles, by their costs where those go by the rows of the group (DW).
+  // the tiles, by their costs where those go by the rows of the group (DW); and of the tail's
+  // slices.
   const int xcd = blockIdx.x & 7;
   int first, last;
-  if constexpr (FORM == DW) {
+  if (g.tail.slices > 1) {
+    first = g.tail.full / 8 * xcd;
+    last = first + g.tail.full / 8;
+    tile_table<NT, BM>(g.g, g.tn, 0, g.most, tab, sh);
+  } else if constexpr (FORM == DW) {
     const int each = (int)((n + BM - 1) / BM) * g.tn * g.slices;
     tile_table<NT, BK>(g.g, 1, kStart * g.slices, 1 << 30, tab, sh);
     first = share_of(tab, g.g.E, each, xcd, 8);
@@ -158,10 +170,14 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
     first = xcd * per;
     last = min(items, first + per);
   }
+  const int parts = g.tail.slices > 1 ? g.tail.rest * g.tail.slices : 0;
+  const int here = max(last - first, 0), tail0 = parts * xcd / 8;
+  const int count = here + parts * (xcd + 1) / 8 - tail0;
 
   struct Tile {
     int e, m0, n0, slice, y;  // group, first row and column of the tile, end of the group's rows
     int64_t x;                // the group's first row
+    int part;                 // of the tail: which one of its sums; -1
   };
   Operand<AC, PA> A;
   Operand<BC, PB> B;
@@ -176,9 +192,15 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
     fs = (fs + 1) & 3;
   };
   // The tile of an item and its operands; false: none (invalid offsets).
-  auto set = [&](int item, Tile& t) {
-    int ti, tj;
+  auto set = [&](int place, Tile& t) {
+    int ti, tj, cut = 0;
     t.slice = 0;
+    t.part = place < here ? -1 : tail0 + place - here;
+    int item = first + place;
+    if (t.part >= 0) {
+      item = g.tail.full + t.part / g.tail.slices;
+      cut = t.part % g.tail.slices;
+    }
     if constexpr (FORM == DW) {  // group by group, slice by slice
       const int tm = (int)((n + BM - 1) / BM), each = tm * g.tn;
       t.e = item / each;
@@ -195,36 +217,44 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
       const int tm = (int)(t.y - t.x + BM - 1) / BM, i = __builtin_amdgcn_readfirstlane(item - tab[t.e]);
       if ((unsigned)i >= (unsigned)(tm * g.tn)) return false;
       tile_at(i, tm, g.tn, ti, tj);
-    } else if (g.slices > 1) {
+    } else if (g.slices > 1 || t.part >= 0) {
       const int c = (int)((t.y - t.x + BK - 1) / BK);  // in whole stages
+      const int of = t.part >= 0 ? g.tail.slices : g.slices, q = t.part >= 0 ? cut : t.slice;
       const int64_t x0 = t.x;
-      t.x = x0 + (int64_t)c * t.slice / g.slices * BK;
-      t.y = (int)min((int64_t)t.y, x0 + (int64_t)c * (t.slice + 1) / g.slices * BK);
+      t.x = x0 + (int64_t)c * q / of * BK;
+      t.y = (int)min((int64_t)t.y, x0 + (int64_t)c * (q + 1) / of * BK);
+    }
+    // FWD, DX: the summed index from k0 on
+    int k0 = 0, k1 = (int)(FORM == FWD ? k : n);
+    if (FORM != DW && t.part >= 0) {
+      const int c = (k1 + BK - 1) / BK;
+      k0 = (int)((int64_t)c * cut / g.tail.slices) * BK;
+      k1 = min(k1, (int)((int64_t)c * (cut + 1) / g.tail.slices) * BK);
     }
     const int m0 = t.m0 = ti * BM, n0 = t.n0 = tj * BN;
     const int rest = (int)(t.y - t.x) - m0;  // FWD, DX: rows of the group from the tile on
     const uint16_t* const we = FORM == DW ? g.b : g.b + t.e * n * k;
     if constexpr (FORM == FWD) {
-      K = (int)k;
+      K = k1 - k0;
       const int64_t f = n >> 1, r0 = t.x + m0;
       if (g.g.source)
-        A.start(g.a, k, [&](int o) -> int64_t {
+        A.start(g.a + k0, k, [&](int o) -> int64_t {
           const int64_t s = o < rest ? source_of(g.g, (int)r0 + o) : -1;
           return s < 0 ? -1 : s * k;
         });
       else
-        A.start(g.a + r0 * k, k, [&](int o) -> int64_t { return o < rest ? o * k : -1; });
+        A.start(g.a + r0 * k + k0, k, [&](int o) -> int64_t { return o < rest ? o * k : -1; });
       if constexpr (GLU)  // 16 columns of the gate, then the same 16 of the other half
-        B.start(we, k, [&](int o) -> int64_t {
+        B.start(we + k0, k, [&](int o) -> int64_t {
           const int64_t c = (n0 >> 1) + (o >> 5) * 16 + (o & 15);
           return c < f ? (c + (o >> 4 & 1) * f) * k : -1;
         });
       else
-        B.start(we + n0 * k, k, [&](int o) -> int64_t { return n0 + o < n ? o * k : -1; });
+        B.start(we + n0 * k + k0, k, [&](int o) -> int64_t { return n0 + o < n ? o * k : -1; });
     } else if constexpr (FORM == DX) {
-      K = (int)n;
-      A.start(g.a + (t.x + m0) * n, n, [&](int o) -> int64_t { return o < rest ? o * n : -1; });
-      B.start(we + n0, k, [&](int c) -> int64_t { return n0 + c < k ? c : -1; });
+      K = k1 - k0;
+      A.start(g.a + (t.x + m0) * n + k0, n, [&](int o) -> int64_t { return o < rest ? o * n : -1; });
+      B.start(we + k0 * k + n0, k, [&](int c) -> int64_t { return n0 + c < k ? c : -1; });
     } else {
       K = (int)(t.y - t.x);
       A.start(g.a + t.x * n + m0, n, [&](int c) -> int64_t { return m0 + c < n ? c : -1; });
@@ -317,10 +347,10 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
   };
 
   Tile t;
-  int item = first + (blockIdx.x >> 3);
+  int item = blockIdx.x >> 3;
   const int stride = gridDim.x >> 3;
   auto next = [&]() {  // sets the next tile and issues its first stage
-    for (; item < last; item += stride) {
+    for (; item < count; item += stride) {
       if (!set(item, t)) continue;
       item += stride;
 #pragma unroll
@@ -417,6 +447,14 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
         };
         // GLU: 16 columns of the gate, 16 of the other half in turn
         const int v = GLU ? (oc >> 4) * 32 + (oc & 15) : oc;
+        if (d.part >= 0) {  // as the products left them
+#pragma unroll
+          for (int q = 0; q < (GLU ? 4 : 2); ++q) {
+            const int col = v + (q & 1) * 4 + (q >> 1) * 16;
+            *(floatx4*)(g.part + ((int64_t)d.part * BM + wm + h * 32 + row) * BN + wn + col) = get(col);
+          }
+          continue;
+        }
         const floatx4 v0 = get(v), v1 = get(v + 4);
         if constexpr (FORM == FWD) {
           if (d.x + o < d.y && c < (GLU ? n >> 1 : n)) {
@@ -448,6 +486,43 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
       __builtin_amdgcn_wave_barrier();
     }
     barrier_lds();  // the stages are free for the next tile
+  }
+}
+
+// The tail's tiles (256 x 256): the sums of their slices, in order, and what the epilogue makes of
+// them.  Block (rows of a tile, tile); eight columns per thread.
+template <int FORM, int ACT>
+__global__ void __launch_bounds__(256) k_tail(const Args g) {
+  constexpr bool GLU = ACT == RFT_ACT_SWIGLU;
+  constexpr int B = 256, LR = (GLU ? B / 2 : B) / 8;  // lanes per row
+  const int64_t n = g.n, k = g.k;
+  const int outer = (int)(((FORM == DW ? n : (int64_t)g.g.rows) + B - 1) / B);
+  int ti, tj;
+  tile_at(g.tail.full + blockIdx.y, outer, g.tn, ti, tj);
+  const int row = blockIdx.x * (256 / LR) + threadIdx.x / LR, oc = (threadIdx.x % LR) * 8;
+  const int64_t r = (int64_t)ti * B + row, c = (int64_t)tj * (GLU ? B / 2 : B) + oc;
+  if (r >= (FORM == DW ? n : (int64_t)g.g.rows) || c >= (FORM != FWD ? k : GLU ? n >> 1 : n)) return;
+  const int v = GLU ? (oc >> 4) * 32 + (oc & 15) : oc;
+  floatx4 s[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) s[q] = (floatx4){0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < g.tail.slices; ++x) {
+    const float* const p = g.part + (((int64_t)blockIdx.y * g.tail.slices + x) * B + row) * B + v;
+    s[0] += *(const floatx4*)p;
+    s[1] += *(const floatx4*)(p + 4);
+    if (GLU) {
+      s[2] += *(const floatx4*)(p + 16);
+      s[3] += *(const floatx4*)(p + 20);
+    }
+  }
+  if constexpr (FORM == FWD) {
+    finish8<ACT>(g.o, 0, n, r, c, s[0], s[1], s[2], s[3]);
+  } else if (FORM == DX || g.dw_bf16) {
+    store8((FORM == DX ? g.dx : (uint16_t*)g.dw) + r * k + c, s[0], s[1]);
+  } else {
+    floatx4* const p = (floatx4*)((float*)g.dw + r * k + c);
+    p[0] = g.accumulate ? p[0] + s[0] : s[0];
+    p[1] = g.accumulate ? p[1] + s[1] : s[1];
   }
 }
 
@@ -645,25 +720,68 @@ hipError_t launch_lin(Args a, int64_t tiles, int64_t across, hipStream_t s) {
   a.most = (int)tiles;
   // a whole round of blocks, a multiple of the XCDs
   const int64_t round = MI == 8 ? 256 : 512;
-  const unsigned grid = (unsigned)std::min<int64_t>(round, ceil_div(tiles, 8) * 8);
+  const int64_t items = a.tail.slices > 1 ? a.tail.full + (int64_t)a.tail.rest * a.tail.slices : tiles;
+  const unsigned grid = (unsigned)std::min<int64_t>(round, ceil_div(items, 8) * 8);
   k_lin<FORM, MI, NJ, ACT><<<grid, NT, 0, s>>>(a);
   return hipGetLastError();
 }
 
-// outer: FWD, DX: rows; DW: n
-template <int FORM, int ACT>
-hipError_t launch_tiles(const Args& a, int64_t outer, int64_t across, hipStream_t s) {
-  auto tiles = [&](int64_t bm, int64_t bn) {
-    return FORM >= DW ? a.g.E * a.slices * ceil_div(outer, bm) * ceil_div(across, bn)
-                      : (outer / bm + a.g.E) * ceil_div(across, bn);
-  };
-  // By rounds; one of small tiles, half the work of one of large ones, takes 0.65 of its time.
+// How a product runs: on tiles of 256 x 256, with a tail, or of 128 x 128.
+struct Plan {
+  bool large;
+  Tail tail;
+  size_t part_bytes;
+};
+// outer: FWD, DX: rows; DW: n.  summed: the summed index; dense: one group of all rows, whose
+// tiles the host can count.
+Plan plan_of(bool dw, const rft_groups& g, int slices, int64_t outer, int64_t across, int64_t summed) {
   auto time = [&](int64_t b, int per) {  // of a group's last tile half is taken to be there
-    return rounds(FORM >= DW ? tiles(b, b) : tiles_expected(outer, a.g.E, b) * ceil_div(across, b), per);
+    const int64_t down = dw ? g.n_groups * slices * ceil_div(outer, b) : tiles_expected(outer, g.n_groups, b);
+    return rounds(down * ceil_div(across, b), per);
   };
-  if (time(256, 1) <= 0.65 * time(128, 2))
-    return launch_lin<FORM, 8, 8, ACT>(a, tiles(256, 256), across, s);
-  return launch_lin<FORM, 4, 4, ACT>(a, tiles(128, 128), across, s);
+  const double small = 0.65 * time(128, 2);  // half the work of a round of large ones in 0.65 of its time
+  double large = time(256, 1);
+  Plan p = {large <= small, {0, 0, 1}, 0};
+  if (g.offsets || slices > 1) return p;
+  // In us: a stage of 64 takes 1.6, a tile 8 more; a slice's sums of a tile 0.12 to write and read,
+  // the launch that adds them 6.
+  const int64_t tiles = ceil_div(outer, 256) * ceil_div(across, 256), nk = ceil_div(summed, BK);
+  const int rest = (int)(tiles % 256);
+  double best = 1.6 * (nk + kStart);
+  const double one = best;
+  int cut = 1;
+  for (int c = 2; c <= 16 && rest > 0 && nk >= 8 * c; ++c) {
+    const double t = ceil_div((int64_t)rest * c, 256) * 1.6 * (ceil_div(nk, c) + kStart) + 0.12 * rest * c + 6;
+    if (t < best) {
+      best = t;
+      cut = c;
+    }
+  }
+  if (cut == 1) return p;
+  large = large - 1 + best / one;
+  p.large = large <= small;
+  if (p.large) {
+    p.tail = {(int)(tiles - rest), rest, cut};
+    p.part_bytes = (size_t)rest * cut * 256 * 256 * 4;
+  }
+  return p;
+}
+
+template <int FORM, int ACT>
+hipError_t launch_tiles(const Plan& p, Args a, int64_t outer, int64_t across, hipStream_t s) {
+  auto tiles = [&](int64_t b) {
+    return FORM >= DW ? a.g.E * a.slices * ceil_div(outer, b) * ceil_div(across, b)
+                      : (outer / b + a.g.E) * ceil_div(across, b);
+  };
+  if (!p.large) return launch_lin<FORM, 4, 4, ACT>(a, tiles(128), across, s);
+  a.tail = p.tail;
+  const hipError_t e = launch_lin<FORM, 8, 8, ACT>(a, tiles(256), across, s);
+  if (e != hipSuccess || p.tail.slices == 1) return e;
+  a.tn = (int)ceil_div(across, 256);
+  constexpr int F = FORM == DWS ? DW : FORM;
+  constexpr int rows = 256 / ((ACT == RFT_ACT_SWIGLU ? 128 : 256) / 8);  // per block
+  k_tail<F, ACT><<<dim3(256 / rows, (unsigned)p.tail.rest), 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 // Slices of a group's rows for d_weight: where its tiles leave CUs idle and the rows are many.
@@ -683,6 +801,8 @@ struct BwdWs {
   double* bias;
   float* dw;
   uint32_t* from;
+  float* part;  // of a tail
+  Plan dx_plan, dw_plan;
   size_t bytes;
 };
 BwdWs carve_bwd(void* base, const rft_groups& g, int dtype, int64_t k, int64_t n, int act) {
@@ -694,6 +814,10 @@ BwdWs carve_bwd(void* base, const rft_groups& g, int dtype, int64_t k, int64_t n
   w.bias = c.take<double>((size_t)std::max(dz_slices(g, m, 1), dz_slices(g, m, 8)) * g.n_groups * n);
   const int s = dw_slices(g, k, n);
   w.dw = s > 1 ? c.take<float>((size_t)s * g.n_groups * n * k) : nullptr;
+  w.dx_plan = plan_of(false, g, 1, g.rows, k, n);
+  w.dw_plan = plan_of(true, g, s, n, k, g.rows);
+  const size_t part = dtype == RFT_BF16 ? std::max(w.dx_plan.part_bytes, w.dw_plan.part_bytes) : 0;
+  w.part = part ? (float*)c.take<char>(part) : nullptr;
   w.from = dtype == RFT_BF16 && g.source ? c.take<uint32_t>((size_t)g.rows + kFromPad) : nullptr;
   w.bytes = c.bytes();
   return w;
@@ -711,7 +835,9 @@ extern "C" {
 size_t rft_linear_workspace_bytes(const rft_groups* groups, int dtype, int64_t k, int64_t n,
                                   int32_t act) {
   if (check_groups("rft_linear_workspace_bytes", groups, dtype, k, n, act)) return 0;
-  return dtype == RFT_BF16 ? linear_few_plan(*groups, k, n, act).ws_bytes : 0;
+  if (dtype != RFT_BF16) return 0;
+  const FewPlan few = linear_few_plan(*groups, k, n, act);
+  return few.fits ? few.ws_bytes : plan_of(false, *groups, 1, groups->rows, n, k).part_bytes;
 }
 
 rft_status rft_linear(const rft_groups* groups, const void* x, const void* weight, int dtype,
@@ -745,7 +871,10 @@ rft_status rft_linear(const rft_groups* groups, const void* x, const void* weigh
   a.n = n;
   a.o = o;
   hipError_t err = hipSuccess;
-  by_act(act, [&](auto A) { err = launch_tiles<FWD, decltype(A)::value>(a, groups->rows, n, s); });
+  a.part = (float*)ws;
+  a.tail.slices = 1;
+  const Plan plan = plan_of(false, *groups, 1, groups->rows, n, k);
+  by_act(act, [&](auto A) { err = launch_tiles<FWD, decltype(A)::value>(plan, a, groups->rows, n, s); });
   RFT_HIP(err, fn);
   return RFT_OK;
 }
@@ -821,10 +950,12 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
   a.n = n;
   a.a = (const uint16_t*)dz;
   a.slices = 1;
+  a.tail.slices = 1;
   if (d_x && any) {
     a.b = (const uint16_t*)weight;
     a.dx = (uint16_t*)d_x;
-    RFT_HIP((launch_tiles<DX, RFT_ACT_NONE>(a, groups->rows, k, s)), fn);
+    a.part = w.part;
+    RFT_HIP((launch_tiles<DX, RFT_ACT_NONE>(w.dx_plan, a, groups->rows, k, s)), fn);
   }
   if (d_weight) {
     a.b = (const uint16_t*)x;
@@ -832,13 +963,14 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
     a.dw_bf16 = dw_dtype == RFT_BF16;
     a.accumulate = accumulate;
     a.slices = slices;
-    a.part = w.dw;
+    a.part = slices > 1 ? w.dw : w.part;
     if (g.source) {
       a.from = w.from;
       k_from<<<(unsigned)ceil_div(g.rows + kFromPad, 256), 256, 0, s>>>(g, k, w.from);
       RFT_HIP(hipGetLastError(), fn);
     }
-    RFT_HIP((g.source ? launch_tiles<DWS, RFT_ACT_NONE>(a, n, k, s) : launch_tiles<DW, RFT_ACT_NONE>(a, n, k, s)), fn);
+    RFT_HIP((g.source ? launch_tiles<DWS, RFT_ACT_NONE>(w.dw_plan, a, n, k, s)
+                      : launch_tiles<DW, RFT_ACT_NONE>(w.dw_plan, a, n, k, s)), fn);
     if (slices > 1) {
       const int64_t count = g.E * n * k;
       k_dw_sum<<<grid_xy(ceil_div(count / 4, 256)), 256, 0, s>>>(w.dw, slices, count, d_weight, a.dw_bf16,

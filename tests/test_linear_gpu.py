@@ -191,6 +191,46 @@ def test_large_tiles():
     check_backward(c)
 
 
+@pytest.mark.parametrize("act", ("none", "swiglu"))
+@pytest.mark.parametrize("rows,k,n", [(4352, 4096, 4096), (4100, 4104, 4352), (2100, 8200, 2064)])
+def test_tail_in_slices(rows, k, n, act):
+    """Dense layers whose last tiles are cut along the summed index, against float64 on the GPU."""
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    r = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+    x, w, b = r(rows, k).to(BF), (r(n, k) / math.sqrt(k)).to(BF), r(n).to(BF)
+    m = n // 2 if act == "swiglu" else n
+    res, dy = r(rows, m).to(BF), r(rows, m).to(BF)
+    y, z = R.rft_linear(x, w, bias=b, act=CODE[act], residual=res, want_z=True)
+    x6, w6 = x.double(), w.double()
+    want = x6 @ w6.T.contiguous() + b.double()
+    eps = 2.0 ** -23
+    tz = (k + 3) * eps * (x6.abs() @ w6.abs().T.contiguous() + b.double().abs())
+    assert bool(((z.double() - want).abs() <= tz + half(BF) * (want.abs() + tz)).all())
+    # y by its own rounding and z's error through slopes of at most 1.13 |u| and |silu(g)|
+    a = M.value(want, act)
+    if act == "swiglu":
+        u = want[:, m:].abs()
+        ty = 1.13 * tz[:, :m] * (u + tz[:, m:]) + want[:, :m].abs() * tz[:, m:] + 2.0 ** -20 * a.abs()
+    else:
+        ty = tz
+    yw = a + res.double()
+    ty = ty + 2.0 ** -22 * (a.abs() + yw.abs())
+    assert bool(((y.double() - yw).abs() <= ty + half(BF) * (yw.abs() + ty)).all())
+    if act != "none":
+        return
+    dw0 = r(n, k)
+    dx, dw, _ = R.rft_linear_bwd(dy, x, w, d_weight=dw0.clone(), accumulate=True)
+    d6 = dy.double()
+    want, t = d6 @ w6, (n + 3) * eps * (d6.abs() @ w6.abs())
+    assert bool(((dx.double() - want).abs() <= t + half(BF) * (want.abs() + t)).all())
+    dT = d6.T.contiguous()
+    want, t = dT @ x6 + dw0.double(), (rows + 4) * eps * (dT.abs() @ x6.abs() + dw0.double().abs())
+    assert bool(((dw.double() - want).abs() <= t).all())
+    only = R.rft_linear_bwd(dy, x, w, want_dx=False)[1]
+    want, t = dT @ x6, (rows + 3) * eps * (dT.abs() @ x6.abs())
+    assert bool(((only.double() - want).abs() <= t + half(BF) * (want.abs() + t)).all())
+
+
 @pytest.mark.parametrize("dt", (BF, F32))
 @pytest.mark.parametrize("act", M.ACTS)
 @pytest.mark.parametrize("counts,spare", GROUPS)
