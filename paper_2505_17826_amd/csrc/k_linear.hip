@@ -618,8 +618,9 @@ __global__ void __launch_bounds__(256) k_dz(const Groups g, const Dz d, int slic
 #pragma unroll
         for (int q = 0; q < V; ++q) {
           if (glu) {
-            const float g1 = dy[x][q] * u[x][q] * silu_slope<BF16>(z[x][q]);
-            u[x][q] = dy[x][q] * silu<BF16>(z[x][q]);
+            const float2 f = silu_both<BF16>(z[x][q]);
+            const float g1 = dy[x][q] * u[x][q] * f.y;
+            u[x][q] = dy[x][q] * f.x;
             if (BIAS) s1[q] += u[x][q];
             dy[x][q] = g1;
           } else if (d.act != RFT_ACT_NONE) {

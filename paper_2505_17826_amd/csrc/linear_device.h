@@ -208,11 +208,14 @@ template <bool FAST>
 __device__ __forceinline__ float silu(float x) {
   return x == -INFINITY ? 0.f : x * sigmoid<FAST>(x);
 }
+// silu(x) and its slope s + x s (1 - s), s the sigmoid, 1 - s = exp(-x) s (no cancellation; 1
+// where exp(-x) overflows); at infinities the limits.
 template <bool FAST>
-__device__ __forceinline__ float silu_slope(float x) {
-  const float s = sigmoid<FAST>(x);
-  // x (1 - s) with 1 - s = s(-x): no cancellation; at infinities the limit
-  return fabsf(x) > FLT_MAX ? s : fmaf(s * x, sigmoid<FAST>(-x), s);
+__device__ __forceinline__ float2 silu_both(float x) {
+  const float e = FAST ? __builtin_amdgcn_exp2f(-x * kLog2e) : expf(-x);
+  const float s = FAST ? __builtin_amdgcn_rcpf(1.f + e) : 1.f / (1.f + e);
+  const float t = e <= FLT_MAX ? e * s : 1.f;
+  return make_float2(x == -INFINITY ? 0.f : x * s, fabsf(x) <= FLT_MAX ? fmaf(s * x, t, s) : s);
 }
 template <bool FAST>
 __device__ __forceinline__ float gelu(float x) {
@@ -230,7 +233,7 @@ __device__ __forceinline__ float act_of(int act, float z) {
 }
 template <bool FAST>
 __device__ __forceinline__ float slope_of(int act, float z) {
-  return act == RFT_ACT_SILU ? silu_slope<FAST>(z) : act == RFT_ACT_GELU ? gelu_slope<FAST>(z) : 1.f;
+  return act == RFT_ACT_SILU ? silu_both<FAST>(z).y : act == RFT_ACT_GELU ? gelu_slope<FAST>(z) : 1.f;
 }
 
 // What a forward writes.
