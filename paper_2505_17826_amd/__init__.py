@@ -954,14 +954,15 @@ class ExpertOrder:
         return int(self.offsets.numel()) - 1
 
     def c(self) -> rft_expert_order:
-        if self.places.dim() != 2:
+        off, slots, places = self.offsets, self.slots, self.places
+        if places.dim() != 2:
             raise TypeError("places: int32 [T, k] expected")
-        dev, (T, k) = self.places.device, self.places.shape
-        _want(dev, self.places, torch.int32, (T, k), "places")
-        _want(dev, self.slots, torch.int32, (T * k,), "slots")
-        _want(dev, self.offsets, torch.int32, (self.offsets.numel(),), "offsets")
-        return rft_expert_order(T, k, self.n_experts, _at(self.offsets), _at(self.slots),
-                                _at(self.places))
+        dev, (T, k), i32 = places.device, places.shape, torch.int32
+        _want(dev, places, i32, (T, k), "places")
+        _want(dev, slots, i32, (T * k,), "slots")
+        _want(dev, off, i32, (off.numel(),), "offsets")
+        return rft_expert_order(T, k, off.numel() - 1, off.data_ptr(), slots.data_ptr(),
+                                places.data_ptr())
 
     def groups(self, gather=False):
         """The rows of an rft_linear over the experts; gather: its x are the tokens' rows."""
@@ -1004,21 +1005,11 @@ def rft_expert_sort(expert_ids, n_experts, out=None, ws=None, stream=None) -> Ex
     return out
 
 
-def _expert_rows(order, named, d):
-    """The order as a C struct, with the arrays of a call checked: (name, tensor, rows)."""
-    o = order.c()
-    dev = order.places.device
-    first = next(t for _, t, _ in named if t is not None)
-    for name, t, rows in named:
-        if t is not None:
-            _want(dev, t, first.dtype, (rows, d), name)
-    return o, dev, _dtype_code(first)
-
-
 def _gates(order, gates, dev):
-    if gates is not None:
-        _want(dev, gates, torch.float32, tuple(order.places.shape), "gates")
-    return _at(gates)
+    if gates is None:
+        return None
+    _want(dev, gates, torch.float32, order.places.shape, "gates")
+    return gates.data_ptr()
 
 
 @_allocates
@@ -1027,12 +1018,16 @@ def rft_expert_gather(order: ExpertOrder, x, gates=None, out=None, stream=None):
     from offsets[E] on are left as they were.  Its gradient is rft_expert_combine."""
     _need_gpu(x)
     T, k = order.places.shape
-    d = x.shape[-1]
+    d, dt, dev = x.shape[-1], x.dtype, x.device
+    o = order.c()
+    _want(dev, x, dt, (T, d), "x")
+    _same_device(dev, ("order", order.places))
     if out is None:
-        out = torch.empty((T * k, d), dtype=x.dtype, device=x.device)
-    o, dev, dt = _expert_rows(order, (("x", x, T), ("out", out, T * k)), d)
-    _call(lib().rft_expert_gather, dev, stream, ctypes.byref(o), _at(x), dt, d,
-          _gates(order, gates, dev), _at(out))
+        out = torch.empty((T * k, d), dtype=dt, device=dev)
+    else:
+        _want(dev, out, dt, (T * k, d), "out")
+    _call(lib().rft_expert_gather, dev, stream, ctypes.byref(o), x.data_ptr(), _dtype_code(x), d,
+          _gates(order, gates, dev), out.data_ptr())
     if stream is not None:
         _used_on(stream, out)
     return out
@@ -1043,13 +1038,18 @@ def rft_expert_combine(order: ExpertOrder, rows, gates=None, residual=None, out=
     """Returns [T, d]: the sum of each token's rows (times their gates), and of the residual."""
     _need_gpu(rows)
     T, k = order.places.shape
-    d = rows.shape[-1]
+    d, dt, dev = rows.shape[-1], rows.dtype, rows.device
+    o = order.c()
+    _want(dev, rows, dt, (T * k, d), "rows")
+    _same_device(dev, ("order", order.places))
+    if residual is not None:
+        _want(dev, residual, dt, (T, d), "residual")
     if out is None:
-        out = torch.empty((T, d), dtype=rows.dtype, device=rows.device)
-    o, dev, dt = _expert_rows(order, (("rows", rows, T * k), ("residual", residual, T),
-                                      ("out", out, T)), d)
-    _call(lib().rft_expert_combine, dev, stream, ctypes.byref(o), _at(rows), dt, d,
-          _gates(order, gates, dev), _at(residual), _at(out))
+        out = torch.empty((T, d), dtype=dt, device=dev)
+    else:
+        _want(dev, out, dt, (T, d), "out")
+    _call(lib().rft_expert_combine, dev, stream, ctypes.byref(o), rows.data_ptr(), _dtype_code(rows), d,
+          _gates(order, gates, dev), _at(residual), out.data_ptr())
     if stream is not None:
         _used_on(stream, out)
     return out
@@ -1062,17 +1062,22 @@ def rft_expert_combine_bwd(order: ExpertOrder, d_out, rows, gates=None, d_rows=N
     on.  rows may be None without d_gates."""
     _need_gpu(d_out)
     T, k = order.places.shape
-    d = d_out.shape[-1]
-    if d_rows is None and want_d_rows:
-        d_rows = torch.empty((T * k, d), dtype=d_out.dtype, device=d_out.device)
-    if d_gates is None and want_d_gates:
-        d_gates = torch.empty((T, k), dtype=torch.float32, device=d_out.device)
-    o, dev, dt = _expert_rows(order, (("d_out", d_out, T), ("rows", rows, T * k),
-                                      ("d_rows", d_rows, T * k)), d)
+    d, dt, dev = d_out.shape[-1], d_out.dtype, d_out.device
+    o = order.c()
+    _want(dev, d_out, dt, (T, d), "d_out")
+    _same_device(dev, ("order", order.places))
+    if rows is not None:
+        _want(dev, rows, dt, (T * k, d), "rows")
+    if d_rows is not None:
+        _want(dev, d_rows, dt, (T * k, d), "d_rows")
+    elif want_d_rows:
+        d_rows = torch.empty((T * k, d), dtype=dt, device=dev)
     if d_gates is not None:
         _want(dev, d_gates, torch.float32, (T, k), "d_gates")
-    _call(lib().rft_expert_combine_bwd, dev, stream, ctypes.byref(o), _at(d_out), _at(rows), dt, d,
-          _gates(order, gates, dev), _at(d_rows), _at(d_gates))
+    elif want_d_gates:
+        d_gates = torch.empty((T, k), dtype=torch.float32, device=dev)
+    _call(lib().rft_expert_combine_bwd, dev, stream, ctypes.byref(o), d_out.data_ptr(), _at(rows),
+          _dtype_code(d_out), d, _gates(order, gates, dev), _at(d_rows), _at(d_gates))
     if stream is not None:
         _used_on(stream, d_rows, d_gates)
     return d_rows, d_gates
@@ -1080,23 +1085,24 @@ def rft_expert_combine_bwd(order: ExpertOrder, d_out, rows, gates=None, d_rows=N
 
 def _linear_groups(groups, x, weight):
     """(C struct, rows, E, n, k) of a linear layer; weight [E, n, k], or [n, k] for one group."""
-    dev = x.device
-    if weight.dim() not in (2, 3) or x.dim() != 2:
+    dev, dt, shape = x.device, x.dtype, weight.shape
+    if len(shape) not in (2, 3) or x.dim() != 2:
         raise TypeError("x: [rows, k], weight: [groups, n, k] or [n, k] expected")
-    E = weight.shape[0] if weight.dim() == 3 else 1
-    n, k = weight.shape[-2:]
-    _want(dev, x, weight.dtype, (x.shape[0], k), "x")
-    _want(dev, weight, weight.dtype, tuple(weight.shape), "weight")
+    E = shape[0] if len(shape) == 3 else 1
+    n, k = shape[-2:]
     rows = x.shape[0]
+    _want(dev, x, dt, (rows, k), "x")
+    _want(dev, weight, dt, shape, "weight")
     if groups is None:
         return rft_groups(rows, E, None, None, 1, 0), rows, E, n, k
-    _want(dev, groups.offsets, torch.int32, (E + 1,), "offsets")
-    src = groups.source
-    if src is not None:
-        rows = src.numel()
-        _want(dev, src, torch.int32, (rows,), "source")
-    return rft_groups(rows, E, _at(groups.offsets), _at(src), groups.source_div,
-                      x.shape[0]), rows, E, n, k
+    off, src = groups.offsets, groups.source
+    _want(dev, off, torch.int32, (E + 1,), "offsets")
+    if src is None:
+        return rft_groups(rows, E, off.data_ptr(), None, 1, 0), rows, E, n, k
+    count = src.numel()
+    _want(dev, src, torch.int32, (count,), "source")
+    return (rft_groups(count, E, off.data_ptr(), src.data_ptr(), groups.source_div, rows), count, E,
+            n, k)
 
 
 @_allocates
@@ -1107,21 +1113,26 @@ def rft_linear(x, weight, bias=None, act=RFT_ACT_NONE, residual=None, groups: Gr
     are left as they were)."""
     _need_gpu(x, weight)
     g, rows, E, n, k = _linear_groups(groups, x, weight)
-    dev, dt = x.device, _dtype_code(x)
+    dev, dtype, dt = x.device, x.dtype, _dtype_code(x)
     m = n // 2 if act == RFT_ACT_SWIGLU else n
     if bias is not None:
-        _want(dev, bias, x.dtype, tuple(weight.shape[:-1]), "bias")
-    out = torch.empty((rows, m), dtype=x.dtype, device=dev) if out is None else out
-    if z is None and want_z:
-        z = torch.empty((rows, n), dtype=x.dtype, device=dev)
-    for name, t, c in (("residual", residual, m), ("out", out, m), ("z", z, n)):
-        if t is not None:
-            _want(dev, t, x.dtype, (rows, c), name)
-    _same_device(dev, ("ws", ws))
+        _want(dev, bias, dtype, weight.shape[:-1], "bias")
+    if residual is not None:
+        _want(dev, residual, dtype, (rows, m), "residual")
+    if out is None:
+        out = torch.empty((rows, m), dtype=dtype, device=dev)
+    else:
+        _want(dev, out, dtype, (rows, m), "out")
+    if z is not None:
+        _want(dev, z, dtype, (rows, n), "z")
+    elif want_z:
+        z = torch.empty((rows, n), dtype=dtype, device=dev)
+    if ws is not None:
+        _same_device(dev, ("ws", ws))
     L, rg = lib(), ctypes.byref(g)
-    ws, nb = _workspace(int(L.rft_linear_workspace_bytes(rg, dt, k, n, act)), dev, ws)
-    _call(L.rft_linear, dev, stream, rg, _at(x), _at(weight), dt, k, n, _at(bias), act,
-          _at(residual), _at(out), _at(z), _at(ws), nb)
+    ws, nb = _workspace(L.rft_linear_workspace_bytes(rg, dt, k, n, act), dev, ws)
+    _call(L.rft_linear, dev, stream, rg, x.data_ptr(), weight.data_ptr(), dt, k, n, _at(bias), act,
+          _at(residual), out.data_ptr(), _at(z), _at(ws), nb)
     if stream is not None:
         _used_on(stream, out, z, ws)
     return out, z
