@@ -23,7 +23,7 @@ namespace lin {
 namespace {
 
 
-enum { FWD = 0, DX = 1, DW = 2, DWS = 3 };  // DWS: DW with a source
+enum { FWD = 0, DX = 1, DW = 2 };
 constexpr int BK = 64, NT = 256;
 constexpr int kStart = 8;  // stages that a tile takes for its start and its stores, about
 
@@ -45,7 +45,6 @@ struct Args {
   int dw_bf16, accumulate;
   int slices;             // DW: of a group's rows; > 1: sums to part [slices, E, n, k]
   float* part;
-  const uint32_t* from;   // DW with a source: byte offsets of the rows of x (k_from)
   Tail tail;              // one group of all rows: sums to part [rest, slices, BM, BN]
 };
 
@@ -132,10 +131,9 @@ __device__ __forceinline__ void read_fragment(const char* s, int o, int ks, int 
 // Tiles of 32 MI x 32 NJ, four waves of 16 MI x 16 NJ, two stages of 64 of the summed index in
 // LDS, each multiplied in two halves of 32.  The fragments of a half are read to registers between
 // the products of the half before it.
-template <int FORM_, int MI, int NJ, int ACT>
+template <int FORM, int MI, int NJ, int ACT>
 __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
-  constexpr bool GLU = ACT == RFT_ACT_SWIGLU, SRC = FORM_ == DWS;
-  constexpr int FORM = SRC ? DW : FORM_;
+  constexpr bool GLU = ACT == RFT_ACT_SWIGLU;
   constexpr int BM = 32 * MI, BN = 32 * NJ;
   constexpr bool AC = FORM == DW, BC = FORM != FWD;  // operands whose summed index is the row
   constexpr int PA = MI, PB = NJ, L = PA + PB;  // loads per wave and stage
@@ -144,7 +142,6 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
   constexpr int PD = MI * NJ;                                         // products
   __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
   __shared__ int tab[kMaxGroups + 1], sh[NT / 64];
-  __shared__ uint32_t ring[SRC ? NT / 64 : 1][4][BK];  // DW with a source: offsets of stages' rows
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = (wid >> 1) * (16 * MI), wn = (wid & 1) * (16 * NJ);
@@ -182,15 +179,6 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
   Operand<AC, PA> A;
   Operand<BC, PB> B;
   int K = 0, left = 0;  // of the summed index: all, and from the stage to load next on
-  const uint32_t places = lds_at(ring[wid]);
-  uint64_t from = 0;    // DW with a source: of the offsets to load next, and their place
-  int fs = 0;
-  // Offsets of the rows of one more stage; they are used a stage later.
-  auto load_from = [&]() {
-    load_lds4(from, places + fs * (BK * 4), lane * 4);
-    from += BK * 4;
-    fs = (fs + 1) & 3;
-  };
   // The tile of an item and its operands; false: none (invalid offsets).
   auto set = [&](int place, Tile& t) {
     int ti, tj, cut = 0;
@@ -258,17 +246,7 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
     } else {
       K = (int)(t.y - t.x);
       A.start(g.a + t.x * n + m0, n, [&](int c) -> int64_t { return m0 + c < n ? c : -1; });
-      B.start(SRC ? we + n0 : we + t.x * k + n0, k, [&](int c) -> int64_t { return n0 + c < k ? c : -1; });
-      if constexpr (SRC) {
-        B.step = 0;
-        from = uniform(g.from + t.x);
-        fs = 0;
-        load_from();
-        load_from();
-        load_from();
-        wait_vm<0>();
-        fs = 0;
-      }
+      B.start(we + t.x * k + n0, k, [&](int c) -> int64_t { return n0 + c < k ? c : -1; });
     }
     left = K;
     return true;
@@ -285,23 +263,9 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
     if (x < PA) {
       A.template load<NOPS>(x, place + st, A.off[x]);
     } else {
-      const int i = x - PA;
-      uint32_t v = B.off[i];
-      if constexpr (SRC) {  // off has the place of the stage's row in consecutive rows
-        const int r = B.at[0] + 4 * i;
-        const uint32_t row = ring[wid][fs][r];
-        v = v != kNone && row != kNone ? v - (uint32_t)r * (uint32_t)(k * 2) + row : kNone;
-      }
-      B.template load<NOPS>(i, place + placeB + st, v);
+      B.template load<NOPS>(x - PA, place + placeB + st, B.off[x - PA]);
     }
-    if (x == L - 1) {
-      left -= BK;
-      if constexpr (SRC) {
-        fs = (fs + 3) & 3;
-        load_from();
-        fs = (fs + 1) & 3;
-      }
-    }
+    if (x == L - 1) left -= BK;
   };
 
   floatx4 acc[MI][NJ];
@@ -368,7 +332,7 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = (floatx4){0.f, 0.f, 0.f, 0.f};
     const int nk = (K + BK - 1) / BK;
-    wait_vm<L + (SRC ? 1 : 0)>();  // stage 0 (and the stores of the tile before)
+    wait_vm<L>();  // stage 0 (and the stores of the tile before)
     barrier_lds();
 #pragma unroll
     for (int x = 0; x < RD; ++x) read_one(0, lds, x);
@@ -526,15 +490,19 @@ __global__ void __launch_bounds__(256) k_tail(const Args g) {
   }
 }
 
-// Byte offsets of the rows of x behind the groups' rows (kNone: zeros), and of kFromPad rows past
-// them, which the stages at the end read.  d_weight's product brings them to LDS a stage before
-// it loads the rows, so no load waits for another.
-constexpr int kFromPad = 8 * BK;
-__global__ void __launch_bounds__(256) k_from(const Groups g, int64_t k, uint32_t* from) {
-  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (r >= (int64_t)g.rows + kFromPad) return;
-  const int64_t s = r < g.rows ? source_of(g, (int)r) : -1;
-  from[r] = s < 0 ? kNone : (uint32_t)(s * k * 2);
+// The rows of x behind the groups' rows, for d_weight's product, which takes 64 of them at a time as
+// they lie in memory; a wave per row and 512 columns.  HBM bounds it: 32 us for 32768 rows of 1536,
+// beside 264 us of their product (64 groups, n = 1536).  Loading the rows where they lie, their
+// offsets brought to LDS a stage ahead, took 280 us for the two, and a second kind of main loop.
+__global__ void __launch_bounds__(256) k_take(const Groups g, const uint16_t* __restrict__ x, int64_t k,
+                                              int64_t units, uint16_t* rows) {
+  const int64_t u = block_index() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r = u / units, c = ((u - r * units) * 64 + (threadIdx.x & 63)) * 8;
+  if (r >= g.rows || c >= k) return;
+  const int64_t s = source_of(g, (int)r);
+  u32x4 v = {0, 0, 0, 0};
+  if (s >= 0) v = *(const u32x4*)(x + s * k + c);
+  *(u32x4*)(rows + r * k + c) = v;
 }
 
 // d_weight from the slices' sums, in order; four elements per thread (count % 4 == 0).
@@ -771,7 +739,7 @@ Plan plan_of(bool dw, const rft_groups& g, int slices, int64_t outer, int64_t ac
 template <int FORM, int ACT>
 hipError_t launch_tiles(const Plan& p, Args a, int64_t outer, int64_t across, hipStream_t s) {
   auto tiles = [&](int64_t b) {
-    return FORM >= DW ? a.g.E * a.slices * ceil_div(outer, b) * ceil_div(across, b)
+    return FORM == DW ? a.g.E * a.slices * ceil_div(outer, b) * ceil_div(across, b)
                       : (outer / b + a.g.E) * ceil_div(across, b);
   };
   if (!p.large) return launch_lin<FORM, 4, 4, ACT>(a, tiles(128), across, s);
@@ -779,9 +747,8 @@ hipError_t launch_tiles(const Plan& p, Args a, int64_t outer, int64_t across, hi
   const hipError_t e = launch_lin<FORM, 8, 8, ACT>(a, tiles(256), across, s);
   if (e != hipSuccess || p.tail.slices == 1) return e;
   a.tn = (int)ceil_div(across, 256);
-  constexpr int F = FORM == DWS ? DW : FORM;
   constexpr int rows = 256 / ((ACT == RFT_ACT_SWIGLU ? 128 : 256) / 8);  // per block
-  k_tail<F, ACT><<<dim3(256 / rows, (unsigned)p.tail.rest), 256, 0, s>>>(a);
+  k_tail<FORM, ACT><<<dim3(256 / rows, (unsigned)p.tail.rest), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -801,7 +768,7 @@ struct BwdWs {
   void* dz;
   double* bias;
   float* dw;
-  uint32_t* from;
+  uint16_t* taken;  // rows of a source
   float* part;  // of a tail
   Plan dx_plan, dw_plan;
   size_t bytes;
@@ -819,7 +786,7 @@ BwdWs carve_bwd(void* base, const rft_groups& g, int dtype, int64_t k, int64_t n
   w.dw_plan = plan_of(true, g, s, n, k, g.rows);
   const size_t part = dtype == RFT_BF16 ? std::max(w.dx_plan.part_bytes, w.dw_plan.part_bytes) : 0;
   w.part = part ? (float*)c.take<char>(part) : nullptr;
-  w.from = dtype == RFT_BF16 && g.source ? c.take<uint32_t>((size_t)g.rows + kFromPad) : nullptr;
+  w.taken = dtype == RFT_BF16 && g.source ? c.take<uint16_t>((size_t)g.rows * k) : nullptr;
   w.bytes = c.bytes();
   return w;
 }
@@ -965,13 +932,13 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
     a.accumulate = accumulate;
     a.slices = slices;
     a.part = slices > 1 ? w.dw : w.part;
-    if (g.source) {
-      a.from = w.from;
-      k_from<<<(unsigned)ceil_div(g.rows + kFromPad, 256), 256, 0, s>>>(g, k, w.from);
+    if (g.source && any) {
+      a.b = w.taken;
+      const int64_t units = ceil_div(k, 512);
+      k_take<<<grid_xy(ceil_div(g.rows * units, 4)), 256, 0, s>>>(g, (const uint16_t*)x, k, units, w.taken);
       RFT_HIP(hipGetLastError(), fn);
     }
-    RFT_HIP((g.source ? launch_tiles<DWS, RFT_ACT_NONE>(w.dw_plan, a, n, k, s)
-                      : launch_tiles<DW, RFT_ACT_NONE>(w.dw_plan, a, n, k, s)), fn);
+    RFT_HIP((launch_tiles<DW, RFT_ACT_NONE>(w.dw_plan, a, n, k, s)), fn);
     if (slices > 1) {
       const int64_t count = g.E * n * k;
       k_dw_sum<<<grid_xy(ceil_div(count / 4, 256)), 256, 0, s>>>(w.dw, slices, count, d_weight, a.dw_bf16,

@@ -160,16 +160,6 @@ __device__ __forceinline__ void load_lds(uint64_t base, uint32_t dst, uint32_t v
                  : "memory", "m0");
 #endif
 }
-// The same with four bytes per lane, to dst + 4 lane.
-__device__ __forceinline__ void load_lds4(uint64_t base, uint32_t dst, uint32_t v) {
-#ifdef __HIP_DEVICE_COMPILE__
-  const u32x4 w = {(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, kSpan, 0x00020000u};
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
-               :
-               : "s"(dst), "v"(v), "s"(w)
-               : "memory", "m0");
-#endif
-}
 __device__ __forceinline__ s16x4 read_tr(const char* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
 }
