@@ -521,8 +521,8 @@ __global__ void __launch_bounds__(256) k_dw_sum(const float* __restrict__ part, 
 }
 
 // ------------------------------------------------------------------ dz and d_bias --
-// Block (columns, group, slice of the group's rows): four waves take its rows in turn, V columns
-// per lane; dz is stored as it is rounded, the bias sums it unrounded: a lane's rows in fp32, the
+// Block (columns, group, slice of the group's rows; without d_bias a slice of all rows, which
+// an uneven load does not make uneven): four waves take its rows in turn, V columns per lane; dz is stored as it is rounded, the bias sums it unrounded: a lane's rows in fp32, the
 // waves and slices in fp64.  HBM bounds it.
 template <bool BF16, int V>
 __device__ __forceinline__ void load_v(const void* p, int64_t at, float (&v)[V]) {
@@ -563,8 +563,9 @@ __global__ void __launch_bounds__(256) k_dz(const Groups g, const Dz d, int slic
   const bool glu = d.act == RFT_ACT_SWIGLU;
   const int64_t m = glu ? d.n / 2 : d.n;
   const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * V;
-  const int2 r = rows_of(g, e);
-  const int64_t cnt = r.y - r.x;
+  // without the bias all groups' rows are one run
+  const int2 r = BIAS ? rows_of(g, e) : make_int2(rows_of(g, 0).x, rows_of(g, g.E - 1).y);
+  const int64_t cnt = max(r.y - r.x, 0);
   const int64_t a = r.x + cnt * slice / slices, b = r.x + cnt * (slice + 1) / slices;
   float s0[V], s1[V];
 #pragma unroll
@@ -881,8 +882,11 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
     const Dz d = {dy, z, d_x || d_weight ? w.dz : nullptr, d_bias, act, accumulate, n};
     const int64_t m = act == RFT_ACT_SWIGLU ? n / 2 : n;
     const bool wide = bf || (m % 4 == 0 && n % 4 == 0 && aligned16(dy) && aligned16(z));
-    const int V = bf ? 8 : wide ? 4 : 1, sl = dz_slices(*groups, m, V);
-    const dim3 grid((unsigned)ceil_div(m, 64 * V), (unsigned)g.E, (unsigned)sl);
+    const int V = bf ? 8 : wide ? 4 : 1;
+    const int64_t across = ceil_div(m, 64 * V);
+    const int sl = d_bias ? dz_slices(*groups, m, V)
+                          : (int)std::max<int64_t>(1, std::min(8192 / across, groups->rows / 8));
+    const dim3 grid((unsigned)across, (unsigned)(d_bias ? g.E : 1), (unsigned)sl);
     auto go = [&](auto B, auto W) {
       constexpr bool bf16 = decltype(B)::value;
       constexpr int v = decltype(W)::value;
