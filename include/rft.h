@@ -701,7 +701,8 @@ typedef enum { RFT_ACT_NONE = 0, RFT_ACT_SILU = 1, RFT_ACT_GELU = 2, RFT_ACT_SWI
 
 /* (host struct holding device pointers) The rows of a product and whose weight
  * each takes: group g (an expert) has rows [offsets[g], offsets[g+1]).  Rows from
- * offsets[n_groups] on belong to none: they are neither read nor written.  offsets
+ * offsets[n_groups] on belong to none: nothing depends on them and results leave
+ * them as they were.  offsets
  * NULL: one group of all rows.  offsets are taken as non-decreasing and inside
  * [0, rows]; others give unspecified values, every access stays in bounds.
  * With source (e.g. an order's slots, and source_div its top_k), row r of x is
@@ -725,7 +726,8 @@ typedef struct {
  * fp32 arithmetic in fp32).  RFT_ACT_GELU is z Phi(z).
  * bf16 needs k % 8 == 0, n % 8 == 0 (n % 16 with RFT_ACT_SWIGLU), 16-byte aligned
  * arrays and, with source, source_rows k < 2^31 - 64; fp32 takes any sizes and
- * alignments.  n k < 2^31 - 64.
+ * alignments.  n k < 2^31 - 64.  y and z overlap none of the other arrays, but for y
+ * with residual.
  * Workspace: rft_linear_workspace_bytes().
  * Errors: RFT_E_NULL, RFT_E_SHAPE, RFT_E_DTYPE, RFT_E_PARAM, RFT_E_WORKSPACE. */
 size_t rft_linear_workspace_bytes(const rft_groups* groups, int dtype, int64_t k, int64_t n,
@@ -744,7 +746,7 @@ rft_status rft_linear(const rft_groups* groups, const void* x, const void* weigh
  * may be NULL.  accumulate != 0: d_weight (RFT_F32) and d_bias are added to; a group
  * without rows has zeros (adds nothing).  With bf16 data the products take dz in
  * bf16 (with RFT_ACT_NONE that is dy itself); d_bias sums it unrounded.
- * Sums run in a fixed order.
+ * Sums run in a fixed order.  Outputs overlap none of the other arrays.
  * Workspace: rft_linear_bwd_workspace_bytes().
  * Errors: as rft_linear. */
 size_t rft_linear_bwd_workspace_bytes(const rft_groups* groups, int dtype, int64_t k, int64_t n,

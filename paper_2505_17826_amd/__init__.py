@@ -973,7 +973,7 @@ class ExpertOrder:
 class Groups:
     """Rows of a product and whose weight each takes: group g has rows [offsets[g],
     offsets[g + 1]).  With source, row r of x is x[source[r] // source_div]."""
-    offsets: torch.Tensor         # int32 [E + 1]
+    offsets: torch.Tensor         # int32 [E + 1]; None: one group of all rows
     source: torch.Tensor = None   # int32 [rows]
     source_div: int = 1
 
@@ -1096,13 +1096,13 @@ def _linear_groups(groups, x, weight):
     if groups is None:
         return rft_groups(rows, E, None, None, 1, 0), rows, E, n, k
     off, src = groups.offsets, groups.source
-    _want(dev, off, torch.int32, (E + 1,), "offsets")
+    if off is not None or E > 1:
+        _want(dev, off, torch.int32, (E + 1,), "offsets")
     if src is None:
-        return rft_groups(rows, E, off.data_ptr(), None, 1, 0), rows, E, n, k
+        return rft_groups(rows, E, _at(off), None, 1, 0), rows, E, n, k
     count = src.numel()
     _want(dev, src, torch.int32, (count,), "source")
-    return (rft_groups(count, E, off.data_ptr(), src.data_ptr(), groups.source_div, rows), count, E,
-            n, k)
+    return (rft_groups(count, E, _at(off), src.data_ptr(), groups.source_div, rows), count, E, n, k)
 
 
 @_allocates

@@ -209,3 +209,31 @@ def test_streams_and_graphs():
         again = call()
         torch.cuda.synchronize()
         assert same(first, held) and same(first, again)
+
+
+def test_past_32_bits():
+    """Rows of more than 2^32 elements: the last tokens' ways to their experts and back."""
+    T, E, k, d = 300_000, 16, 8, 2048
+    g = torch.Generator(device=DEV).manual_seed(2)
+    ids = torch.randint(0, E, (T, k), generator=g, device=DEV, dtype=torch.int32)
+    x = torch.randn(T, d, generator=g, device=DEV, dtype=BF)
+    gates = torch.rand(T, k, generator=g, device=DEV)
+    o = R.rft_expert_sort(ids, E)
+    flat = ids.reshape(-1).long()
+    order = torch.sort(flat, stable=True)[1]
+    assert torch.equal(o.slots.long(), order)
+    assert torch.equal(o.places.reshape(-1).long()[order], torch.arange(T * k, device=DEV))
+    rows = R.rft_expert_gather(o, x)
+    last = torch.tensor([0, 1, T * k // 2, T * k - 2, T * k - 1], device=DEV)
+    assert torch.equal(rows[last], x[order[last] // k])
+    at = slice(T - 200, T)
+    out = R.rft_expert_combine(o, rows, gates=gates)
+    want = gates[at].double().sum(1, keepdim=True) * x[at].double()
+    tol = (k + 2) * 2.0 ** -24 * want.abs()
+    assert bool(((out[at].double() - want).abs() <= tol + torch.finfo(BF).eps / 2 * (want.abs() + tol)).all())
+    d_rows, d_gates = R.rft_expert_combine_bwd(o, x, rows, gates=gates, d_rows=rows)
+    want = x[at].double().square().sum(1, keepdim=True).expand(200, k)
+    assert bool(((d_gates[at].double() - want).abs() <= (d + 2) * 2.0 ** -24 * want).all())
+    s = order[last]
+    want = gates.reshape(-1)[s, None].double() * x[s // k].double()
+    assert bool(((d_rows[last].double() - want).abs() <= (torch.finfo(BF).eps / 2 + 2.0 ** -24) * want.abs()).all())

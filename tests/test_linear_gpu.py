@@ -330,6 +330,44 @@ def test_no_rows_and_no_tokens():
     assert dx.shape == (0, 8) and not dw.any() and not db.any()
 
 
+@pytest.mark.parametrize("dt", (BF, F32))
+def test_rows_before_the_first_group(dt):
+    c = Case([15, 0, 13], 72, 80, "silu", dt, seed=3)
+    x, dy = torch.cat([torch.full((5, 72), math.nan, dtype=dt), c.x]), torch.cat([torch.full((5, 80), math.nan, dtype=dt), c.dy])
+    g = R.Groups(torch.tensor([5, 20, 20, 33], dtype=torch.int32, device=DEV))
+    y0 = torch.full((33, 80), 7.0, dtype=dt, device=DEV)
+    y, z = R.rft_linear(x.to(DEV), c.w.to(DEV), act=R.RFT_ACT_SILU, groups=g, out=y0, want_z=True)
+    y1, z1 = R.rft_linear(c.x.to(DEV), c.w.to(DEV), act=R.RFT_ACT_SILU, groups=c.groups(), want_z=True)
+    assert torch.equal(y[5:], y1) and bool((y[:5] == 7).all())
+    d0 = torch.full((33, 72), 7.0, dtype=dt, device=DEV)
+    a = R.rft_linear_bwd(dy.to(DEV), x.to(DEV), c.w.to(DEV), z=z, act=R.RFT_ACT_SILU, groups=g, d_x=d0, want_db=True)
+    b = R.rft_linear_bwd(c.dy.to(DEV), c.x.to(DEV), c.w.to(DEV), z=z1, act=R.RFT_ACT_SILU, groups=c.groups(), want_db=True)
+    assert torch.equal(a[0][5:], b[0]) and bool((a[0][:5] == 7).all())
+    # the rows of a group are summed in the same order wherever they lie
+    assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+    only = R.rft_linear_bwd(dy.to(DEV), x.to(DEV), c.w.to(DEV), z=z, act=R.RFT_ACT_SILU, groups=g)[1]
+    assert torch.equal(only, b[1])
+
+
+@pytest.mark.parametrize("dt", (BF, F32))
+def test_one_group_with_a_source(dt):
+    """A dense layer of chosen rows; of no rows at all, where the bias is left."""
+    g = torch.Generator().manual_seed(4)
+    x, w, b = (torch.randn(*s, generator=g).to(dt) for s in ((30, 64), (48, 64), (48,)))
+    for count in (7, 300):
+        src = torch.randint(0, 30, (count,), generator=g, dtype=torch.int32)
+        groups = R.Groups(None, src.to(DEV))
+        y, _ = R.rft_linear(x.to(DEV), w.to(DEV), groups=groups)
+        same, _ = R.rft_linear(x[src.long()].to(DEV), w.to(DEV))
+        assert torch.equal(y, same)
+        dw = R.rft_linear_bwd(y, x.to(DEV), w.to(DEV), groups=groups, want_dx=False)[1]
+        assert torch.equal(dw, R.rft_linear_bwd(y, x[src.long()].to(DEV), w.to(DEV), want_dx=False)[1])
+        none = torch.empty(0, 64, dtype=dt, device=DEV)
+        y, _ = R.rft_linear(none, w.to(DEV), bias=b.to(DEV), groups=groups)
+        assert torch.equal(y.cpu(), b.expand(count, 48))
+        assert not R.rft_linear_bwd(y, none, w.to(DEV), groups=groups, want_dx=False)[1].any()
+
+
 def test_offsets_that_are_not_valid_stay_inside():
     """Offsets that decrease or leave the rows: unspecified values, but only the rows' places."""
     for dt in (BF, F32):
@@ -446,3 +484,32 @@ def test_streams_graphs_and_repeats():
         x.mul_(-1) if i == 0 else None
         if i == 0:
             first = call()
+
+
+def test_past_32_bits():
+    """x of more than 2^32 bytes, dense and in groups: rows at its end, and the sums over all of it."""
+    rows, k, n = 1_150_000, 2048, 16
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(rows, k, generator=g, device=DEV, dtype=BF)
+    w = (torch.randn(2, n, k, generator=g, device=DEV) / math.sqrt(k)).to(BF)
+    dy = torch.randn(rows, n, generator=g, device=DEV).to(BF)
+    cut = 1_100_001
+    groups = R.Groups(torch.tensor([0, cut, rows], dtype=torch.int32, device=DEV))
+    y, _ = R.rft_linear(x, w, groups=groups)
+    dx, dw, db = R.rft_linear_bwd(dy, x, w, groups=groups, dw_dtype=F32, want_db=True)
+    for a, b, e in ((0, 300, 0), (cut - 300, cut, 0), (cut, cut + 300, 1), (rows - 300, rows, 1)):
+        x6, w6, d6 = x[a:b].double(), w[e].double(), dy[a:b].double()
+        for got, want, mag, terms in ((y[a:b], x6 @ w6.T.contiguous(), x6.abs() @ w6.abs().T.contiguous(), k),
+                                      (dx[a:b], d6 @ w6, d6.abs() @ w6.abs(), n)):
+            t = (terms + 3) * 2.0 ** -23 * mag
+            assert bool(((got.double() - want).abs() <= t + half(BF) * (want.abs() + t)).all()), (a, e)
+    for e, (a, b) in enumerate(((0, cut), (cut, rows))):
+        want, mag = torch.zeros(n, k, dtype=torch.float64, device=DEV), torch.zeros((), device=DEV)
+        for i in range(a, b, 100_000):
+            j = min(b, i + 100_000)
+            want += dy[i:j].double().T.contiguous() @ x[i:j].double()
+        # 2^20 products of unit size summed in fp32: sums of up to a few 2^10, whose roundings (2^-23
+        # of them, 2^15 of the matrix instruction) add up like sqrt(2^15) at random; ten times that
+        assert float((dw[e].double() - want).abs().max()) <= 10 * 2 ** 12 * 2.0 ** -23 * 2 ** 7.5
+        s = dy[a:b].double().sum(0)
+        assert bool(((db[e].double() - s).abs() <= 2.0 ** -23 * dy[a:b].double().abs().sum(0)).all())
