@@ -10,11 +10,14 @@
 // slots, 64 at a time; lanes with the same expert find each other by one ballot per bit of the
 // id, so a slot's rank in its expert is the wave's count before it plus the lanes below.  The
 // wave's counts start from those of the waves and blocks before it: no atomic decides an order.
-// Latency bounds it: the ids are 4 bytes per slot, the order 8.
+// Latency bounds it: the ids are 4 bytes per slot, the order 8 (1600 slots 4.8 us, 8192 8.4 us
+// in one block, 524288 in three launches of 4.6, 4.6 and 10 us).
 //
 // Rows move as 16 bytes per lane where size and alignment allow it, else element by element;
 // HBM bounds them.  The gather goes by tokens, not by sorted rows: a token's row is read once
 // and written to its k places, where going by sorted rows reads it k times, far apart in time.
+// 65536 tokens (41000 with experts), k = 8, 1536 bf16 (1 GB of rows): gather 220 us,
+// combine 285 (the least 228), combine_bwd 400; the whole case 4.85 TB/s, a copy 5.25.
 #include <algorithm>
 
 #include "abi_common.h"

@@ -13,6 +13,15 @@
 //
 // The groups' sizes are on the device.  A block makes the table of tiles per group in LDS and
 // walks its share of all tiles, so a launch has no empty blocks and the host waits for nothing.
+//
+// The matrix pipe bounds the products, and what feeds it: a 256 x 256 tile (the largest whose
+// sums fit the registers, so the fewest bytes per product) brings 64 KiB per stage to each CU.
+// Waves of 128 x 128 read 32 KiB of fragments per stage from LDS, waves of 64 x 128 48 KiB; with
+// one wave to a SIMD nothing hides a wait, so reads and loads are laid out by hand between the
+// products.  Measured at 16384 x 4096 x 8256, in turn with a library product: 828 us (1.34 PFLOP/s)
+// against 708; with zeros for data 709 and 572.  Copies without the main loop's loads (the products
+// on what LDS held) took 632 where the whole took 831, without the reads and barriers too 521: the
+// loads cost most, in waits, in power or in both, which was not told apart.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,7 +30,6 @@
 namespace rft {
 namespace lin {
 namespace {
-
 
 enum { FWD = 0, DX = 1, DW = 2 };
 constexpr int BK = 64, NT = 256;
@@ -522,8 +530,9 @@ __global__ void __launch_bounds__(256) k_dw_sum(const float* __restrict__ part, 
 
 // ------------------------------------------------------------------ dz and d_bias --
 // Block (columns, group, slice of the group's rows; without d_bias a slice of all rows, which
-// an uneven load does not make uneven): four waves take its rows in turn, V columns per lane; dz is stored as it is rounded, the bias sums it unrounded: a lane's rows in fp32, the
-// waves and slices in fp64.  HBM bounds it.
+// an uneven load does not make uneven: 111 -> 58 us at 32768 rows, n = 1536, RFT_ACT_SWIGLU, 252
+// MB): four waves take its rows in turn, V columns per lane; dz is stored as it is rounded, the
+// bias sums it unrounded: a lane's rows in fp32, the waves and slices in fp64.  HBM bounds it.
 template <bool BF16, int V>
 __device__ __forceinline__ void load_v(const void* p, int64_t at, float (&v)[V]) {
   if constexpr (V == 1) {
@@ -727,7 +736,9 @@ Plan plan_of(bool dw, const rft_groups& g, int slices, int64_t outer, int64_t ac
       cut = c;
     }
   }
-  if (cut == 1) return p;
+  // Small gains are the model's, not the card's: 16384 x 18944 x 3584 (128 tiles over, 0.92) 1752 us
+  // cut, 1729 whole; 16384 x 3584 x 18944 (0.59) 1604 and 1736; 16384 x 4224 x 4096 (0.65) 448, 468.
+  if (best > 0.85 * one) return p;
   large = large - 1 + best / one;
   p.large = large <= small;
   if (p.large) {
