@@ -486,6 +486,44 @@ def test_streams_graphs_and_repeats():
             first = call()
 
 
+def test_tail_of_chosen_rows_in_a_graph():
+    """One group of chosen rows whose last tiles are cut (272 tiles of 256 x 256): the bits of the rows
+    gathered first, eager and from a graph replayed with other rows."""
+    rows, k, n = 4352, 4096, 4096
+    g = torch.Generator(device=DEV).manual_seed(11)
+    r = lambda *s: torch.randn(*s, generator=g, device=DEV).to(BF)  # noqa: E731
+    x, w, dy = r(1500, k), (r(n, k) / 64), r(rows, n)
+    src = torch.randint(0, 1500, (rows,), generator=g, dtype=torch.int32, device=DEV)
+    groups = R.Groups(None, src)
+
+    def call():
+        y, _ = R.rft_linear(x, w, groups=groups)
+        dx, dw, _ = R.rft_linear_bwd(dy, x, w, groups=groups)
+        return y, dx, dw
+
+    def gathered():
+        rows_ = x[src.long()]
+        y, _ = R.rft_linear(rows_, w)
+        dx, dw, _ = R.rft_linear_bwd(dy, rows_, w)
+        return y, dx, dw
+
+    for a, b in zip(call(), gathered()):
+        assert torch.equal(a, b)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for i in range(3):
+        src.copy_(torch.randint(0, 1500, (rows,), generator=g, dtype=torch.int32, device=DEV))
+        for t in held:
+            t.zero_()
+        graph.replay()
+        want = gathered()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b), i
+
+
 def test_past_32_bits():
     """x of more than 2^32 bytes, dense and in groups: rows at its end, and the sums over all of it."""
     rows, k, n = 1_150_000, 2048, 16
