@@ -709,7 +709,7 @@ typedef enum { RFT_ACT_NONE = 0, RFT_ACT_SILU = 1, RFT_ACT_GELU = 2, RFT_ACT_SWI
  * x[source[r] div source_div], and x has source_rows rows; a source outside them
  * is a row of zeros.  Without, x has `rows` rows. */
 typedef struct {
-  int64_t rows;            /* < 2^31                                               */
+  int64_t rows;            /* <= 2^31 - 512                                        */
   int32_t n_groups;        /* 1 .. 1024                                            */
   const int32_t* offsets;  /* [n_groups + 1], or NULL (n_groups 1)                 */
   const int32_t* source;   /* [rows], or NULL                                      */

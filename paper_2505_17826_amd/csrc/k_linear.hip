@@ -166,7 +166,7 @@ __global__ void __launch_bounds__(NT, MI == 8 ? 1 : 2) k_lin(const Args g) {
     tile_table<NT, BM>(g.g, g.tn, 0, g.most, tab, sh);
   } else if constexpr (FORM == DW) {
     const int each = (int)((n + BM - 1) / BM) * g.tn * g.slices;
-    tile_table<NT, BK>(g.g, 1, kStart * g.slices, 1 << 30, tab, sh);
+    tile_table<NT, BK>(g.g, 1, kStart * g.slices, kMostItems, tab, sh);
     first = share_of(tab, g.g.E, each, xcd, 8);
     last = share_of(tab, g.g.E, each, xcd + 1, 8);
   } else {
@@ -653,8 +653,8 @@ Groups groups_of(const rft_groups& g) {
 
 rft_status check_groups(const char* fn, const rft_groups* g, int dtype, int64_t k, int64_t n, int act) {
   if (!g) return fail(RFT_E_NULL, "%s: groups is NULL", fn);
-  if (g->rows < 0 || g->rows >= ((int64_t)1 << 31))
-    return fail(RFT_E_SHAPE, "%s: rows=%lld must be in [0, 2^31)", fn, (long long)g->rows);
+  if (g->rows < 0 || g->rows > kMostRows)
+    return fail(RFT_E_SHAPE, "%s: rows=%lld must be in [0, 2^31 - 512]", fn, (long long)g->rows);
   if (g->n_groups < 1 || g->n_groups > kMaxGroups)
     return fail(RFT_E_SHAPE, "%s: n_groups=%d must be in [1, %d]", fn, g->n_groups, kMaxGroups);
   if (!g->offsets && g->n_groups != 1) return fail(RFT_E_NULL, "%s: groups.offsets is NULL", fn);
@@ -680,7 +680,7 @@ rft_status check_groups(const char* fn, const rft_groups* g, int dtype, int64_t 
                   (long long)(g->source_rows * k));
   }
   // tiles are counted in 32 bits
-  if ((g->rows / 64 + g->n_groups) * (ceil_div(std::max(k, n), 64) + 1) >= ((int64_t)1 << 30))
+  if ((g->rows / 64 + g->n_groups) * (ceil_div(std::max(k, n), 64) + 1) > kMostItems)
     return fail(RFT_E_SHAPE, "%s: rows=%lld with k=%lld, n=%lld are more than one call takes", fn,
                 (long long)g->rows, (long long)k, (long long)n);
   return RFT_OK;
