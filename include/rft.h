@@ -57,7 +57,7 @@
 extern "C" {
 #endif
 
-#define RFT_ABI_VERSION 9
+#define RFT_ABI_VERSION 10
 
 typedef enum {
   RFT_OK = 0,
@@ -736,6 +736,8 @@ rft_status rft_linear(const rft_groups* groups, const void* x, const void* weigh
                       int64_t k, int64_t n, const void* bias, int32_t act, const void* residual,
                       void* y, void* z, void* ws, size_t ws_bytes, void* stream);
 
+enum { RFT_ONE_PRODUCT = 0x100 }; /* with RFT_F32 as dw_dtype of rft_linear_bwd */
+
 /* Gradients of rft_linear (that of the residual is dy itself):
  *   dz = dy act'(z), d_x[r] = dz[r] weight_g, d_weight_g = sum_r dz[r]^T x[r],
  *   d_bias_g = sum_r dz[r].
@@ -745,7 +747,9 @@ rft_status rft_linear(const rft_groups* groups, const void* x, const void* weigh
  * [n_groups, n, k] in dw_dtype (RFT_F32 or `dtype`), d_bias [n_groups, n] f32; each
  * may be NULL.  accumulate != 0: d_weight (RFT_F32) and d_bias are added to; a group
  * without rows has zeros (adds nothing).  With bf16 data the products take dz in
- * bf16 (with RFT_ACT_NONE that is dy itself); d_bias sums it unrounded.
+ * bf16 (with RFT_ACT_NONE that is dy itself); d_bias sums it unrounded.  A d_weight
+ * in fp32 takes the rest of dz too, as a second bf16 value in a second product (2^-16 of
+ * each term instead of 2^-8); dw_dtype RFT_F32 | RFT_ONE_PRODUCT leaves that out.
  * Sums run in a fixed order.  Outputs overlap none of the other arrays.
  * Workspace: rft_linear_bwd_workspace_bytes().
  * Errors: as rft_linear. */

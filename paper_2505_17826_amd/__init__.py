@@ -29,6 +29,7 @@ RFT_ADV_GRPO, RFT_ADV_MEAN_CENTER, RFT_ADV_LEAVE_ONE_OUT = 0, 1, 2
 RFT_BALANCE_BATCH, RFT_BALANCE_ROLLOUT = 0, 1
 RFT_ACT_NONE, RFT_ACT_SILU, RFT_ACT_GELU, RFT_ACT_SWIGLU = range(4)
 RFT_PRODUCTS_BY_TYPE, RFT_PRODUCTS_ONE, RFT_PRODUCTS_THREE = 0, 1, 3
+RFT_ONE_PRODUCT = 0x100
 (RFT_OP_TOKEN_LOGPROBS, RFT_OP_TOKEN_LOGPROBS_FROM_LOGITS, RFT_OP_PPO_FWD, RFT_OP_PPO_BWD,
  RFT_OP_PPO_BWD_LOGITS, RFT_OP_PPO_FUSED_LOGITS, RFT_OP_PPO_STEP, RFT_OP_SFT_FWD,
  RFT_OP_DPO_FWD) = range(9)
@@ -1141,10 +1142,12 @@ def rft_linear(x, weight, bias=None, act=RFT_ACT_NONE, residual=None, groups: Gr
 @_allocates
 def rft_linear_bwd(dy, x, weight, z=None, act=RFT_ACT_NONE, groups: Groups = None, want_dx=True,
                    want_dw=True, want_db=False, d_x=None, d_weight=None, d_bias=None, dw_dtype=None,
-                   accumulate=False, ws=None, stream=None):
+                   accumulate=False, ws=None, stream=None, one_product=False):
     """Returns (d_x, d_weight, d_bias), None where not wanted.  d_weight has dw_dtype (default:
     the weight's), d_bias is fp32; accumulate adds to the d_weight (fp32) and d_bias given.  With
-    groups.source d_x has the groups' rows; rft_expert_combine sums those of a token."""
+    groups.source d_x has the groups' rows; rft_expert_combine sums those of a token.  On bf16 data
+    an fp32 d_weight behind an activation is made of two products (dz in two bf16 parts);
+    one_product: of one, with dz in bf16."""
     _need_gpu(dy, x, weight)
     g, rows, E, n, k = _linear_groups(groups, x, weight)
     dev, dt = x.device, _dtype_code(x)
@@ -1166,6 +1169,8 @@ def rft_linear_bwd(dy, x, weight, z=None, act=RFT_ACT_NONE, groups: Groups = Non
             raise TypeError("d_weight has another dtype than dw_dtype")
         _want(dev, d_weight, d_weight.dtype, tuple(weight.shape), "d_weight")
         dwt = _dtype_code(d_weight)
+        if one_product and dwt == RFT_F32:
+            dwt |= RFT_ONE_PRODUCT
     if d_bias is not None:
         _want(dev, d_bias, torch.float32, tuple(weight.shape[:-1]), "d_bias")
     _same_device(dev, ("ws", ws))

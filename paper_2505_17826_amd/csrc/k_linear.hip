@@ -531,8 +531,14 @@ __global__ void __launch_bounds__(256) k_dw_sum(const float* __restrict__ part, 
 // ------------------------------------------------------------------ dz and d_bias --
 // Block (columns, group, slice of the group's rows; without d_bias a slice of all rows, which
 // an uneven load does not make uneven: 111 -> 58 us at 32768 rows, n = 1536, RFT_ACT_SWIGLU, 252
-// MB): four waves take its rows in turn, V columns per lane; dz is stored as it is rounded, the
-// bias sums it unrounded: a lane's rows in fp32, the waves and slices in fp64.  HBM bounds it.
+// MB): four waves take its rows in turn, V columns per lane; the bias sums dz unrounded: a lane's
+// rows in fp32, the waves and slices in fp64.  HBM bounds it.
+// On bf16 data dz is stored in bf16, as the matrix instruction takes it.  For results in bf16 that
+// is an error of the size of their own rounding (2.35e-3 from 64 bits in all, 1.66e-3 with dz kept
+// in fp32) and half the products of the alternative.  d_weight in fp32 would have it as its only
+// error, so there d.rest asks for what the rounding left, also in bf16, and the product is made of
+// both: 2^-16 of dz, at 1067 us for the backward of 64 experts (32768 rows, 1536 x 1536, with
+// d_x) where one product takes 552.  (A dz that bf16 holds as no finite value has no rest.)
 template <bool BF16, int V>
 __device__ __forceinline__ void load_v(const void* p, int64_t at, float (&v)[V]) {
   if constexpr (V == 1) {
@@ -561,6 +567,15 @@ __device__ __forceinline__ void store_v(void* p, int64_t at, const float (&v)[V]
     store8((uint16_t*)p + at, (floatx4){v[0], v[1], v[2], v[3]}, (floatx4){v[4], v[5], v[6], v[7]});
   } else {
     *(floatx4*)((float*)p + at) = (floatx4){v[0], v[1], v[2], v[3]};
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void take_rest(float (&v)[V]) {
+#pragma unroll
+  for (int q = 0; q < V; ++q) {
+    const float h = bf16_to_f32(f32_to_bf16(v[q]));
+    v[q] = fabsf(h) <= FLT_MAX ? v[q] - h : 0.f;
   }
 }
 
@@ -605,6 +620,10 @@ __global__ void __launch_bounds__(256) k_dz(const Groups g, const Dz d, int slic
             dy[x][q] *= slope_of<BF16>(d.act, z[x][q]);
           }
           if (BIAS) s0[q] += dy[x][q];
+        }
+        if (BF16 && !BIAS && d.rest) {
+          take_rest(dy[x]);
+          if (glu) take_rest(u[x]);
         }
         if (d.dz) {
           store_v<BF16, V>(d.dz, i * d.n + c, dy[x]);
@@ -872,6 +891,8 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
   const char* fn = "rft_linear_bwd";
   rft_status st = check_groups(fn, groups, dtype, k, n, act);
   if (st) return st;
+  const bool one = dw_dtype == (RFT_F32 | RFT_ONE_PRODUCT);
+  if (one) dw_dtype = RFT_F32;
   if (d_weight && dw_dtype != RFT_F32 && dw_dtype != dtype)
     return fail(RFT_E_DTYPE, "%s: dw_dtype %d is neither fp32 nor the data's", fn, dw_dtype);
   if (d_weight && accumulate && dw_dtype != RFT_F32)
@@ -889,19 +910,20 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
   hipStream_t s = (hipStream_t)stream;
   const bool bf = dtype == RFT_BF16;
   const void* dz = act == RFT_ACT_NONE ? dy : w.dz;
-  if (d_bias || ((d_x || d_weight) && act != RFT_ACT_NONE)) {
-    const Dz d = {dy, z, d_x || d_weight ? w.dz : nullptr, d_bias, act, accumulate, n};
+  // dz (or what its rounding left) to the workspace, and the bias's gradient (or nullptr)
+  auto pass = [&](float* db, int rest) -> rft_status {
+    const Dz d = {dy, z, d_x || d_weight ? w.dz : nullptr, db, act, accumulate, rest, n};
     const int64_t m = act == RFT_ACT_SWIGLU ? n / 2 : n;
     const bool wide = bf || (m % 4 == 0 && n % 4 == 0 && aligned16(dy) && aligned16(z));
     const int V = bf ? 8 : wide ? 4 : 1;
     const int64_t across = ceil_div(m, 64 * V);
-    const int sl = d_bias ? dz_slices(*groups, m, V)
-                          : (int)std::max<int64_t>(1, std::min(8192 / across, groups->rows / 8));
-    const dim3 grid((unsigned)across, (unsigned)(d_bias ? g.E : 1), (unsigned)sl);
+    const int sl = db ? dz_slices(*groups, m, V)
+                      : (int)std::max<int64_t>(1, std::min(8192 / across, groups->rows / 8));
+    const dim3 grid((unsigned)across, (unsigned)(db ? g.E : 1), (unsigned)sl);
     auto go = [&](auto B, auto W) {
       constexpr bool bf16 = decltype(B)::value;
       constexpr int v = decltype(W)::value;
-      if (d_bias)
+      if (db)
         k_dz<bf16, v, true><<<grid, 256, 0, s>>>(g, d, sl, w.bias);
       else
         k_dz<bf16, v, false><<<grid, 256, 0, s>>>(g, d, sl, w.bias);
@@ -913,11 +935,14 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
     else
       go(std::false_type{}, std::integral_constant<int, 1>{});
     RFT_HIP(hipGetLastError(), fn);
-    if (d_bias && sl > 1) {
-      k_bias_sum<<<(unsigned)ceil_div(g.E * n, 256), 256, 0, s>>>(w.bias, sl, g.E * n, d_bias, accumulate);
+    if (db && sl > 1) {
+      k_bias_sum<<<(unsigned)ceil_div(g.E * n, 256), 256, 0, s>>>(w.bias, sl, g.E * n, db, accumulate);
       RFT_HIP(hipGetLastError(), fn);
     }
-  }
+    return RFT_OK;
+  };
+  if (d_bias || ((d_x || d_weight) && act != RFT_ACT_NONE))
+    if ((st = pass(d_bias, 0))) return st;
   const int slices = dw_slices(*groups, k, n);
   if (!bf) {
     if (d_x && any)
@@ -953,12 +978,19 @@ rft_status rft_linear_bwd(const rft_groups* groups, const void* dy, const void* 
       k_take<<<grid_xy(ceil_div(g.rows * units, 4)), 256, 0, s>>>(g, (const uint16_t*)x, k, units, w.taken);
       RFT_HIP(hipGetLastError(), fn);
     }
-    RFT_HIP((launch_tiles<DW, RFT_ACT_NONE>(w.dw_plan, a, n, k, s)), fn);
-    if (slices > 1) {
-      const int64_t count = g.E * n * k;
-      k_dw_sum<<<grid_xy(ceil_div(count / 4, 256)), 256, 0, s>>>(w.dw, slices, count, d_weight, a.dw_bf16,
-                                                               accumulate);
-      RFT_HIP(hipGetLastError(), fn);
+    const int parts = any && act != RFT_ACT_NONE && dw_dtype == RFT_F32 && !one ? 2 : 1;
+    for (int part = 0; part < parts; ++part) {
+      if (part > 0) {  // in the place of dz, which d_x and the first product have read
+        if ((st = pass(nullptr, 1))) return st;
+        a.accumulate = 1;
+      }
+      RFT_HIP((launch_tiles<DW, RFT_ACT_NONE>(w.dw_plan, a, n, k, s)), fn);
+      if (slices > 1) {
+        const int64_t count = g.E * n * k;
+        k_dw_sum<<<grid_xy(ceil_div(count / 4, 256)), 256, 0, s>>>(w.dw, slices, count, d_weight, a.dw_bf16,
+                                                                 a.accumulate);
+        RFT_HIP(hipGetLastError(), fn);
+      }
     }
   }
   return RFT_OK;

@@ -236,6 +236,7 @@ struct Dz {
   void* dz;       // nullptr: only the bias
   float* d_bias;  // nullptr: only dz
   int act, accumulate;
+  int rest;       // 1: not dz, but what its rounding left
   int64_t n;
 };
 
