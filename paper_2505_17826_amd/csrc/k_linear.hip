@@ -531,8 +531,9 @@ __global__ void __launch_bounds__(256) k_dw_sum(const float* __restrict__ part, 
 // ------------------------------------------------------------------ dz and d_bias --
 // Block (columns, group, slice of the group's rows; without d_bias a slice of all rows, which
 // an uneven load does not make uneven: 111 -> 58 us at 32768 rows, n = 1536, RFT_ACT_SWIGLU, 252
-// MB): four waves take its rows in turn, V columns per lane; the bias sums dz unrounded: a lane's
-// rows in fp32, the waves and slices in fp64.  HBM bounds it.
+// MB): four waves take its rows in turn, V columns per lane; the bias sums dz unrounded: up to
+// kRunRows of a lane's rows in fp32 (terms that are alike round the same way at every step), all
+// else in fp64.  HBM bounds it.
 // On bf16 data dz is stored in bf16, as the matrix instruction takes it.  For results in bf16 that
 // is an error of the size of their own rounding (2.35e-3 from 64 bits in all, 1.66e-3 with dz kept
 // in fp32) and half the products of the alternative.  d_weight in fp32 would have it as its only
@@ -579,6 +580,7 @@ __device__ __forceinline__ void take_rest(float (&v)[V]) {
   }
 }
 
+constexpr int kRunRows = 128;
 template <bool BF16, int V, bool BIAS>
 __global__ void __launch_bounds__(256) k_dz(const Groups g, const Dz d, int slices, double* part) {
   constexpr int R = V == 1 ? 4 : 2;  // rows whose loads are under way
@@ -594,8 +596,26 @@ __global__ void __launch_bounds__(256) k_dz(const Groups g, const Dz d, int slic
   float s0[V], s1[V];
 #pragma unroll
   for (int q = 0; q < V; ++q) s0[q] = s1[q] = 0.f;
+  // what the lane has joined (in registers: 100 us for 8192 rows of 18944 bf16, 87 so)
+  __shared__ double sum[4][2][BIAS ? 64 * V : 1];
+  auto join = [&](bool first) {
+#pragma unroll
+    for (int q = 0; q < V; ++q) {
+      double &t0 = sum[w][0][q * 64 + lane], &t1 = sum[w][1][q * 64 + lane];
+      t0 = first ? s0[q] : t0 + s0[q];
+      t1 = first ? s1[q] : t1 + s1[q];
+      s0[q] = s1[q] = 0.f;
+    }
+  };
+  bool joined = false;
+  int run = 0;
   if (c < m) {
     for (int64_t i0 = a + w; i0 < b; i0 += 4 * R) {
+      if (BIAS && (run += R) > kRunRows) {
+        join(!joined);
+        joined = true;
+        run = R;
+      }
       float dy[R][V], z[R][V], u[R][V];
 #pragma unroll
       for (int x = 0; x < R; ++x) {
@@ -633,18 +653,13 @@ __global__ void __launch_bounds__(256) k_dz(const Groups g, const Dz d, int slic
     }
   }
   if constexpr (!BIAS) return;
-  __shared__ float sum[4][2][BIAS ? 64 * V : 1];
-#pragma unroll
-  for (int q = 0; q < V; ++q) {
-    sum[w][0][q * 64 + lane] = s0[q];
-    sum[w][1][q * 64 + lane] = s1[q];
-  }
+  join(!joined);
   __syncthreads();
   for (int i = threadIdx.x; i < 128 * V; i += 256) {
     const int half = i / (64 * V), j = i % (64 * V);
     const int64_t col = ((int64_t)blockIdx.x * 64 + j % 64) * V + j / 64;
     if (col >= m || (half && !glu)) continue;
-    const double t = ((double)sum[0][half][j] + sum[1][half][j]) + ((double)sum[2][half][j] + sum[3][half][j]);
+    const double t = (sum[0][half][j] + sum[1][half][j]) + (sum[2][half][j] + sum[3][half][j]);
     const int64_t at = e * d.n + half * m + col;
     if (slices > 1)
       part[(int64_t)slice * g.E * d.n + at] = t;
