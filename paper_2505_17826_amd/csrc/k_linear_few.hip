@@ -1,8 +1,10 @@
 // Linear layers on bf16 data with few rows per group: single tokens, decode steps.
 //
-// The weights are read once and each value multiplies a few rows, so HBM bounds it.  A block
-// owns 64 columns (RFT_ACT_SWIGLU: 32 of each half) of one group that has rows, and takes its
-// rows 16 MT at a time.  Stages of 128 of the summed index go straight to LDS, NS - 1 of them on
+// A group's weight is read once for every 16 MT of its rows (a pass), which for most groups is once,
+// so HBM bounds it.  A block owns 64 columns (RFT_ACT_SWIGLU: 32 of each half) of one pass; there
+// are as many blocks as groups, and where a few groups hold many rows all blocks take their
+// passes (2560 rows on one of 64 groups of 1536 x 1536 30 us; walked by the group's own blocks
+// alone 332).  Stages of 128 of the summed index go straight to LDS, NS - 1 of them on
 // their way: what keeps HBM busy is bytes in flight, and those in LDS cost no registers.
 // (Weights straight to registers in the matrix instruction's layout, 64 bytes of 16 rows per
 // load, and the summed index dealt to the waves reached 2.8 TB/s.)  Where the blocks are few
@@ -10,6 +12,8 @@
 // Measured: 24 rows, k = 18944, n = 3584 (136 MB of weights) 23 us and 4.4 for the sums; 1600
 // rows over 64 groups, 1536 x 1536 (302 MB) 68 us, 4.4 TB/s (a copy reaches 5.2); 8 rows of 8
 // groups of 128 (38 MB) 9.5 us.
+#include <limits.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -19,33 +23,60 @@ namespace rft {
 namespace lin {
 namespace {
 
-// The i-th group that has rows; -1: none.  By whole waves.
-__device__ __forceinline__ int nth_group(const Groups& g, int i) {
-  if (!g.offsets) return i == 0 && g.rows > 0 ? 0 : -1;
+// A group's rows are taken R at a time, in passes; those of all groups are in one row.  Pass `item`:
+// its group (-1: there are no more), its first row and the end of the group's; and how many passes
+// there are.  By whole waves.
+struct Pass {
+  int e, from, end, total;
+};
+template <int R, int Q>  // of up to 64 Q groups
+__device__ __forceinline__ Pass pass_of_groups(const Groups& g, int item) {
+  // all groups' offsets are on their way before the first is looked at
   const int lane = threadIdx.x & 63;
-  for (int e0 = 0; e0 < g.E; e0 += 256) {
-    uint64_t m[4];
+  const uint64_t below = (1ull << lane) - 1;
+  int first[Q], end[Q];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int e = e0 + q * 64 + lane;
-      bool some = false;
-      if (e < g.E) {
-        const int2 r = rows_of(g, e);
-        some = r.y > r.x;
-      }
-      m[q] = __builtin_amdgcn_ballot_w64(some);
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int c = __builtin_popcountll(m[q]);
-      if (i < c) {
-        const bool me = (m[q] >> lane & 1) && __builtin_popcountll(m[q] & ((1ull << lane) - 1)) == i;
-        return e0 + q * 64 + (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(me));
-      }
-      i -= c;
+  for (int q = 0; q < Q; ++q) {
+    first[q] = end[q] = 0;
+    if (q * 64 < g.E) {
+      const int e = min(q * 64 + lane, g.E - 1);
+      first[q] = g.offsets[e];
+      end[q] = g.offsets[e + 1];
     }
   }
-  return -1;
+  Pass f = {-1, 0, 0, 0};
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    if (q * 64 >= g.E) break;
+    const int x = min(max(first[q], 0), g.rows), y = min(max(end[q], x), g.rows);
+    const int p = q * 64 + lane < g.E ? (y - x + R - 1) / R : 0;
+    // passes of the groups before, by the bits of their counts: most have one or none
+    int before = 0, all = 0;
+    for (int b = 0;; ++b) {
+      const uint64_t m = __builtin_amdgcn_ballot_w64((p >> b) & 1);
+      before += __builtin_popcountll(m & below) << b;
+      all += __builtin_popcountll(m) << b;
+      if (!__builtin_amdgcn_ballot_w64((p >> b) > 1)) break;
+    }
+    const int i = item - f.total;
+    const uint64_t me = __builtin_amdgcn_ballot_w64(before <= i && i < before + p);
+    if (me) {
+      const int at = __builtin_ctzll(me);
+      f.e = q * 64 + at;
+      f.from = __builtin_amdgcn_readlane(x, at) + (i - __builtin_amdgcn_readlane(before, at)) * R;
+      f.end = __builtin_amdgcn_readlane(y, at);
+    }
+    f.total += all;
+  }
+  return f;
+}
+template <int R>
+__device__ __forceinline__ Pass pass_at(const Groups& g, int item) {
+  if (!g.offsets) {
+    const int total = (g.rows + R - 1) / R;
+    return {item < total ? 0 : -1, item * R, g.rows, total};
+  }
+  return g.E <= 128 ? pass_of_groups<R, 2>(g, item) : pass_of_groups<R, kMaxGroups / 64>(g, item);
 }
 
 struct Few {
@@ -73,9 +104,6 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, q4 = lane >> 4;
   const uint32_t place = lds_at(lds);
-  const int e = nth_group(f.g, blockIdx.y);
-  if (e < 0) return;
-  const int2 rows = rows_of(f.g, e);
   const int64_t half = f.n >> 1, m = GLU ? half : f.n, c0 = (int64_t)blockIdx.x * (GLU ? BN / 2 : BN);
   // this block's share of the summed index
   const int all = (int)((f.k + BK - 1) / BK);
@@ -83,7 +111,6 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
   const int nk = s1 - s0;
   // wave w loads columns 16 w .. of the tile: GLU: the gate's and the other half's 16 in turn
   const int64_t col = GLU ? c0 + (wave >> 1) * 16 : c0 + wave * 16;
-  const uint64_t wbase = uniform(f.w + (e * f.n + (GLU && (wave & 1) ? half : 0) + col) * f.k + (int64_t)s0 * BK);
   uint32_t woff[4];
   int wk[4];
 #pragma unroll
@@ -94,13 +121,19 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
   }
   const int xk = (r16 ^ (wave * 4 + q4)) * 8;
   const int K = (int)f.k - s0 * BK;
-  for (int r0 = rows.x; r0 < rows.y; r0 += MT * 16) {
+  for (int item = blockIdx.y, total = INT_MAX; item < total; item += gridDim.y) {
+    const Pass pass = pass_at<MT * 16>(f.g, item);
+    const int e = pass.e;
+    if (e < 0) return;
+    total = pass.total;
+    const int r0 = pass.from, rows_end = pass.end;
+    const uint64_t wbase = uniform(f.w + (e * f.n + (GLU && (wave & 1) ? half : 0) + col) * f.k + (int64_t)s0 * BK);
     const uint64_t xbase = uniform((f.g.source ? f.x : f.x + r0 * f.k) + (int64_t)s0 * BK);
     uint32_t xoff[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int r = r0 + i * 16 + wave * 4 + q4;
-      const int64_t s = r >= rows.y ? -1 : f.g.source ? source_of(f.g, r) : r - r0;
+      const int64_t s = r >= rows_end ? -1 : f.g.source ? source_of(f.g, r) : r - r0;
       xoff[i] = s < 0 ? kNone : (uint32_t)((s * f.k + xk) * 2);
     }
     auto load = [&](int t) {
@@ -151,7 +184,7 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int64_t r = r0 + i * 16 + r16, c = col + q4 * 4;
-        if (r < rows.y && c < m)
+        if (r < rows_end && c < m)
           *(floatx4*)(f.part + ((int64_t)blockIdx.z * f.g.rows + r) * f.n + (GLU && (wave & 1) ? half : 0) + c) = acc[i];
       }
       continue;
@@ -167,7 +200,7 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           const int64_t r = r0 + i * 16 + r16, c = col + q4 * 4;
-          if (r < rows.y && c < m) finish<ACT>(f.o, e, f.n, r, c, acc[i], other[i * 64 + lane]);
+          if (r < rows_end && c < m) finish<ACT>(f.o, e, f.n, r, c, acc[i], other[i * 64 + lane]);
         }
       }
       __syncthreads();
@@ -175,7 +208,7 @@ __global__ void __launch_bounds__(NT) k_few(const Few f) {
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
         const int64_t r = r0 + i * 16 + r16, c = col + q4 * 4;
-        if (r < rows.y && c < m) finish<ACT>(f.o, e, f.n, r, c, acc[i], acc[i]);
+        if (r < rows_end && c < m) finish<ACT>(f.o, e, f.n, r, c, acc[i], acc[i]);
       }
     }
   }
@@ -217,8 +250,8 @@ FewPlan linear_few_plan(const rft_groups& g, int64_t k, int64_t n, int act) {
   // and 79, 64 rows 92 and 67; one group, 3584 x 4096: 128 rows 21 and 30, 256 rows 32 and 30,
   // 3584 x 18944: 64 rows 31 and 31, 128 rows 60 and 33.
   p.fits = (average <= 40 || (average <= 128 && blocks < 128)) && g.rows <= 65535;
-  // A group with more rows than a block takes at a time has its weight read again: with an uneven
-  // load of 25 rows on average 57 us at four tiles, 66 at two.
+  // A group with more rows than a pass has its weight read again: with an uneven load of 25 rows
+  // on average 57 us at four tiles, 66 at two.
   const int64_t likely = g.n_groups == 1 ? g.rows : 2 * average;
   p.tiles = likely <= 16 ? 1 : likely <= 32 ? 2 : 4;
   p.slices = 1;
