@@ -9,9 +9,9 @@
 // (Weights straight to registers in the matrix instruction's layout, 64 bytes of 16 rows per
 // load, and the summed index dealt to the waves reached 2.8 TB/s.)  Where the blocks are few
 // the summed index is cut into slices, whose sums k_few_sum adds in order.
-// Measured: 24 rows, k = 18944, n = 3584 (136 MB of weights) 23 us and 4.4 for the sums; 1600
-// rows over 64 groups, 1536 x 1536 (302 MB) 68 us, 4.4 TB/s (a copy reaches 5.2); 8 rows of 8
-// groups of 128 (38 MB) 9.5 us.
+// Measured: 24 rows, k = 18944, n = 3584 (136 MB of weights) 23 us and 4.2 for the sums; 1600
+// rows over 64 groups, 1536 x 1536 (302 MB) 65 us, 4.7 TB/s (a copy reaches 5.1); 8 rows of 8
+// groups of 128 (38 MB) 8.8 us.
 #include <limits.h>
 
 #include <algorithm>

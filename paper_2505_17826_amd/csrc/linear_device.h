@@ -75,8 +75,8 @@ __device__ __forceinline__ float sigmoid(float x) {
 }
 // Phi by the complementary error function: 1 + erf(x) would cancel for x < 0.  FAST: with a =
 // |x| / sqrt 2 and t = 1 / (1 + a / 2), erfc(a) = t exp(p(t) - a^2), p fitted to ln(erfc(a)
-// exp(a^2) / t) on a in [0, 10.5] by weighted least squares (2.5e-7; 1.7e-6 with the roundings
-// for |x| < 4).
+// exp(a^2) / t) on a in [0, 10.5] by weighted least squares.  Relative error with these
+// coefficients 3.2e-7 in exact arithmetic, 2.0e-6 with fp32's roundings for |x| < 4.
 template <bool FAST>
 __device__ __forceinline__ float phi_cdf(float x) {
   if (!FAST) return 0.5f * erfcf(-x * 0.70710678f);
