@@ -749,7 +749,8 @@ enum { RFT_ONE_PRODUCT = 0x100 }; /* with RFT_F32 as dw_dtype of rft_linear_bwd 
  * without rows has zeros (adds nothing).  With bf16 data the products take dz in
  * bf16 (with RFT_ACT_NONE that is dy itself); d_bias sums it unrounded.  A d_weight
  * in fp32 takes the rest of dz too, as a second bf16 value in a second product (2^-16 of
- * each term instead of 2^-8); dw_dtype RFT_F32 | RFT_ONE_PRODUCT leaves that out.
+ * each term instead of 2^-8; an infinite x gives NaN); dw_dtype RFT_F32 | RFT_ONE_PRODUCT
+ * leaves that out.
  * Sums run in a fixed order.  Outputs overlap none of the other arrays.
  * Workspace: rft_linear_bwd_workspace_bytes().
  * Errors: as rft_linear. */
